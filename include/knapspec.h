@@ -437,6 +437,97 @@ ks_status ks_spec_accept(const int32_t* p_ids, const float* p_probs, const int32
 ks_status ks_sample_uniforms(uint64_t seed, const int32_t* pos, int n, int purpose, float* out,
                              void* stream);
 
+/* ---- paged cache ---------------------------------------------------------- */
+/*
+ * One layer's cache of keys and values in pages, shared by many sequences.  All
+ * buffers are device memory of the caller, 16-byte aligned:
+ *   k        [n_pages][hkv][page][hd]           keys, token-major
+ *   v        [n_pages][hkv][page / 16][hd][16]  values, in granules of 16 tokens,
+ *                                               dimension-major inside a granule
+ *   k_scale, v_scale  float32 [n_pages][hkv][page / block]  (KS_E4M3; else unused)
+ * kind KS_BF16: bf16 elements.  kind KS_E4M3: 8-bit floats (e4m3, largest value
+ * 448, one NaN code, no infinities); an element is its code times the scale of its
+ * block of `block` tokens and its head.  Scales are powers of two.  page is a power
+ * of two in [16, 1024]; block (KS_E4M3) a power of two in [16, page]; hd is 64 or
+ * 128; n_pages * page * hkv * hd may exceed 2^32.
+ */
+enum { KS_E4M3 = 2 };
+typedef struct ks_paged_cache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int n_pages, page, block;
+  int hkv, hd, kind;
+} ks_paged_cache;
+/*
+ * The rows of a call: B sequences side by side, sequence b the rows
+ * row_start[b] .. row_start[b+1] - 1 of the call's tensors, its row i at position
+ * pos0[b] + i.  Position p lies in page table[b][p / page].  The arrays are device
+ * memory and may change between replays of a captured call; max_rows (rows of one
+ * sequence) and max_len (positions) are what the host promises of them.  Rows
+ * behind row_start[B] are neither read nor written.  A row at a negative position
+ * is padding: nothing is stored for it and it attends nothing.
+ * What the arrays hold beyond the promises is left out, never followed: a page id
+ * outside [0, n_pages) (its tokens are not stored, and not attended), positions at
+ * or past max_len or table_ld * page, rows past max_rows.  Such a sequence's err[b]
+ * is set to 1; err (device int32[B], or NULL) is never cleared.
+ * Sequences may share pages that none of them appends to.  Two calls that append
+ * to one page at the same time, or a table that names a page twice, leave the
+ * shared tokens with either value.
+ */
+typedef struct ks_paged_rows {
+  int B;
+  int rows;                 /* rows of the call's tensors */
+  const int32_t* row_start; /* device [B + 1], ascending */
+  const int32_t* pos0;      /* device [B] */
+  const int32_t* table;     /* device [B][table_ld] */
+  int table_ld;
+  int max_rows;
+  int max_len;
+  int32_t* err;             /* device [B] or NULL */
+} ks_paged_rows;
+/*
+ * ks_paged_append: stores the keys and values of new rows, rotating keys (and
+ * queries) on the way: the pair (f, f + hd/2) of a head by the angle of its
+ * position, rope[p][f] = (cos, sin), device float32 [rope_rows][hd/2][2]; NULL: no
+ * rotation.  Rows at or past rope_rows are treated as past max_len.  k, v
+ * [rows][hkv][hd] and q, q_out [rows][hq][hd] are of dtype (KS_F32 or KS_BF16),
+ * rows ldk, ldv, ldq, ldqo elements apart (a fused projection's rows do); q may be
+ * NULL (then hq, ldq, q_out, ldqo are not looked at), and q_out may equal q (with
+ * ldqo = ldq).  q_out is 0 for padding and for rows past rope_rows.
+ * KS_E4M3: a block's scale is the smallest power of two s (at least 2^-100) with
+ * every finite new |element| <= 448 s, or the scale it has, if it holds earlier
+ * tokens of the sequence (those below pos0[b]) and that is larger; if it grows, their
+ * codes are rounded to the new scale.  Codes are rounded to nearest, ties to even;
+ * an element that is not finite becomes NaN.  Tokens of a block at or past the new
+ * ones have undefined codes.  Appending the same rows again stores the same.
+ * Asynchronous on stream.
+ */
+ks_status ks_paged_append(const ks_paged_cache* cache, const ks_paged_rows* rows, const void* q,
+                          size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv,
+                          void* q_out, size_t ldqo, int hq, int dtype, const float* rope,
+                          int rope_rows, void* stream);
+/*
+ * ks_paged_attention: out = softmax(scale q k^T) v of every row over the positions
+ * 0 .. its own of its sequence, query head h on kv head h / (hq / hkv); hq / hkv <=
+ * 128.  q and out [rows][hq][hd] of dtype, rows ldq and ldo elements apart, 16-byte
+ * aligned (ldq and ldo too).  KS_F32: to float32 precision; KS_BF16: probabilities
+ * are rounded to bf16 before they meet the values.  A row that attends nothing (at
+ * a negative position, or all of its pages invalid) gets zeros, and lse -inf.  Values
+ * and keys past a row's position do not reach it, whatever they hold.  lse: float32
+ * [rows][hq] or NULL, log of the sum of exp(scale q.k).  scale must be finite.
+ * workspace: ks_paged_attention_workspace_bytes() bytes; nothing in it needs to
+ * start at any value, and calls (or captured graphs) that may run at the same time
+ * need one each.  Asynchronous on stream.
+ */
+size_t ks_paged_attention_workspace_bytes(const ks_paged_cache* cache, int B, int rows, int hq,
+                                          int max_rows, int max_len);
+ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* rows,
+                             const void* q, size_t ldq, void* out, size_t ldo, int hq, int dtype,
+                             float scale, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream);
+
 /* Kernel classes of the decode step, for ks_profile_decode. */
 enum {
   KS_KC_EMBED = 0,    /* embedding gather */

@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("KNAPSPEC_LIB") or os.path.join(HERE, "libknapspec.so")
 
 KS_OK, KS_EINVAL, KS_ENOMEM, KS_ECAPACITY, KS_ESTATE, KS_EHIP = 0, -1, -2, -3, -4, -5
-KS_F32, KS_BF16 = 0, 1
+KS_F32, KS_BF16, KS_E4M3 = 0, 1, 2
 KS_QUANT_PAPER_MIN, KS_QUANT_BINS = 0, 1
 KS_MAX_SUBLAYERS = 256
 
@@ -75,6 +75,18 @@ KS_SAMPLE_KMAX = 128
 class Sampling(C.Structure):
     _fields_ = [("temperature", C.c_float), ("top_k", C.c_int), ("top_p", C.c_float),
                 ("seed", C.c_uint64)]
+
+
+class PagedCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p), ("n_pages", C.c_int), ("page", C.c_int),
+                ("block", C.c_int), ("hkv", C.c_int), ("hd", C.c_int), ("kind", C.c_int)]
+
+
+class PagedRows(C.Structure):
+    _fields_ = [("B", C.c_int), ("rows", C.c_int), ("row_start", C.c_void_p),
+                ("pos0", C.c_void_p), ("table", C.c_void_p), ("table_ld", C.c_int),
+                ("max_rows", C.c_int), ("max_len", C.c_int), ("err", C.c_void_p)]
 
 
 class GenStats(C.Structure):
@@ -145,6 +157,12 @@ _SIG = {
                                       _P, _P, _P]),
     "ks_spec_accept": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, C.c_uint64, _I, _P, _P]),
     "ks_sample_uniforms": (_I, [C.c_uint64, _P, _I, _I, _P, _P]),
+    "ks_paged_append": (_I, [C.POINTER(PagedCache), C.POINTER(PagedRows), _P, C.c_size_t, _P,
+                             C.c_size_t, _P, C.c_size_t, _P, C.c_size_t, _I, _I, _P, _I, _P]),
+    "ks_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PagedCache), _I, _I, _I, _I,
+                                                        _I]),
+    "ks_paged_attention": (_I, [C.POINTER(PagedCache), C.POINTER(PagedRows), _P, C.c_size_t, _P,
+                                C.c_size_t, _I, _I, C.c_float, _P, _P, C.c_size_t, _P]),
     "ks_profile_decode": (_I, [_P, _P, _I, _I, C.POINTER(KernelProfile)]),
     "ks_time_launches": (_I, [_P, _P]),
     "ks_sublayer_apply": (_I, [_P, _I, _P, _P, _P, _I, _I]),
@@ -204,6 +222,9 @@ ks_sample_filter_noalloc = _wrap("ks_sample_filter_noalloc")
 ks_spec_accept = _wrap("ks_spec_accept")
 ks_sample_uniforms = _wrap("ks_sample_uniforms")
 ks_sample_workspace_bytes = lib.ks_sample_workspace_bytes
+ks_paged_append = _wrap("ks_paged_append")
+ks_paged_attention = _wrap("ks_paged_attention")
+ks_paged_attention_workspace_bytes = lib.ks_paged_attention_workspace_bytes
 ks_profile_decode = _wrap("ks_profile_decode")
 ks_time_launches = _wrap("ks_time_launches")
 ks_sublayer_apply = _wrap("ks_sublayer_apply")

@@ -1017,6 +1017,139 @@ ks_status ks_sample_uniforms(uint64_t seed, const int32_t* pos, int n, int purpo
   return KS_OK;
 }
 
+static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+static ks_status check_paged(const ks_paged_cache* c, const ks_paged_rows* r, ks::PagedCache& pc,
+                             ks::PagedRows& pr) {
+  REQ(c && r, "null pointer");
+  REQ(c->kind == KS_BF16 || c->kind == KS_E4M3, "a paged cache holds KS_BF16 or KS_E4M3");
+  REQ(c->hd == 64 || c->hd == 128, "hd of a paged cache must be 64 or 128");
+  REQ(c->hkv >= 1 && c->n_pages >= 1, "hkv and n_pages must be positive");
+  REQ(c->page >= 16 && c->page <= 1024 && (c->page & (c->page - 1)) == 0,
+      "page must be a power of two in [16, 1024]");
+  const bool e4 = c->kind == KS_E4M3;
+  REQ(!e4 || (c->block >= 16 && c->block <= c->page && (c->block & (c->block - 1)) == 0),
+      "block must be a power of two in [16, page]");
+  REQ(r->B >= 0 && r->rows >= 0, "B and rows must be >= 0");
+  REQ(r->rows <= 1 << 30 && r->B <= 1 << 20, "too many rows or sequences");
+  if (r->B == 0 || r->rows == 0) return KS_OK;
+  REQ(c->k && c->v && (!e4 || (c->k_scale && c->v_scale)), "null cache pointer");
+  REQ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0, "cache buffers must be 16-byte aligned");
+  REQ(r->row_start && r->pos0 && r->table, "null pointer");
+  REQ(r->table_ld >= 1, "table_ld must be positive");
+  REQ(r->max_rows >= 1 && r->max_len >= 1, "max_rows and max_len must be positive");
+  pc = ks::PagedCache{c->k, c->v, c->k_scale, c->v_scale, c->n_pages, c->page, log2_of(c->page),
+                      e4 ? c->block : 16, e4 ? log2_of(c->block) : 4, c->hkv, c->hd, c->kind};
+  const long long most = std::min((long long)r->table_ld * c->page, 1ll << 30);
+  pr = ks::PagedRows{r->B, r->rows, r->row_start, r->pos0, r->table, r->table_ld,
+                     std::min(r->max_rows, r->rows), (int)std::min<long long>(r->max_len, most),
+                     r->err};
+  return KS_OK;
+}
+
+static bool aligned_rows(const void* p, size_t ld, int dtype) {
+  const size_t es = dtype == KS_BF16 ? 2 : 4;
+  return ((uintptr_t)p & 15) == 0 && (ld * es) % 16 == 0;
+}
+
+ks_status ks_paged_append(const ks_paged_cache* cache, const ks_paged_rows* rows, const void* q,
+                          size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv,
+                          void* q_out, size_t ldqo, int hq, int dtype, const float* rope,
+                          int rope_rows, void* stream) {
+  ks::PagedAppend a{};
+  const ks_status s = check_paged(cache, rows, a.cache, a.rows);
+  if (s != KS_OK) return s;
+  REQ(dtype == KS_F32 || dtype == KS_BF16, "dtype must be KS_F32 or KS_BF16");
+  REQ(!rope || rope_rows >= 1, "rope_rows must be positive");
+  if (rows->B == 0 || rows->rows == 0) return KS_OK;
+  REQ(k && v, "null pointer");
+  const size_t kw = (size_t)cache->hkv * cache->hd;
+  REQ(ldk >= kw && ldv >= kw, "ldk and ldv must hold a row of keys and values");
+  REQ(((uintptr_t)rope & 7) == 0, "rope must be 8-byte aligned");
+  if (q) {
+    REQ(q_out, "null pointer");
+    REQ(hq >= 1, "hq must be positive");
+    REQ(ldq >= (size_t)hq * cache->hd && ldqo >= (size_t)hq * cache->hd,
+        "ldq and ldqo must hold a row of queries");
+    REQ(q != q_out || ldq == ldqo, "rotation in place needs ldqo = ldq");
+  }
+  const long long wgs =
+      (long long)rows->B * cache->hkv * (a.rows.max_rows / 16 + 2) + (long long)rows->rows * hq;
+  REQ(!q || wgs < (1ll << 31), "too many rows and heads for one launch");
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.ldq = ldq;
+  a.ldk = ldk;
+  a.ldv = ldv;
+  a.ldqo = ldqo;
+  a.hq = hq;
+  a.dtype = dtype;
+  a.rope = rope;
+  a.rope_rows = rope_rows;
+  ks::paged_append(a, (hipStream_t)stream);
+  HIPCHK(hipGetLastError());
+  return KS_OK;
+}
+
+size_t ks_paged_attention_workspace_bytes(const ks_paged_cache* cache, int B, int rows, int hq,
+                                          int max_rows, int max_len) {
+  if (!cache || cache->hkv < 1 || (cache->hd != 64 && cache->hd != 128) || B < 0 || rows < 0 ||
+      hq < cache->hkv || hq % cache->hkv || max_rows < 1 || max_len < 1)
+    return 0;
+  if (B == 0 || rows == 0) return 256;
+  const int ns = ks::paged_splits(B, cache->hkv, hq / cache->hkv, std::min(max_rows, rows), max_len);
+  return ns > 1 ? (size_t)rows * hq * ns * (cache->hd + 2) * 4 : 256;
+}
+
+ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* rows,
+                             const void* q, size_t ldq, void* out, size_t ldo, int hq, int dtype,
+                             float scale, float* lse, void* workspace, size_t workspace_bytes,
+                             void* stream) {
+  ks::PagedAttn a{};
+  const ks_status s = check_paged(cache, rows, a.cache, a.rows);
+  if (s != KS_OK) return s;
+  REQ(dtype == KS_F32 || dtype == KS_BF16, "dtype must be KS_F32 or KS_BF16");
+  REQ(hq >= 1 && hq % cache->hkv == 0, "hq must be a multiple of hkv");
+  REQ(hq / cache->hkv <= 128, "query heads per kv head must be <= 128");
+  REQ(std::isfinite(scale), "scale must be finite");
+  if (rows->B == 0 || rows->rows == 0) return KS_OK;
+  REQ(q && out, "null pointer");
+  REQ(ldq >= (size_t)hq * cache->hd && ldo >= (size_t)hq * cache->hd,
+      "ldq and ldo must hold a row of queries");
+  REQ(aligned_rows(q, ldq, dtype) && aligned_rows(out, ldo, dtype),
+      "rows of q and out must be 16-byte aligned");
+  const int G = hq / cache->hkv;
+  const int len = std::max(1, rows->max_len);
+  const int ns = ks::paged_splits(rows->B, cache->hkv, G, a.rows.max_rows, len);
+  REQ((long long)ns * cache->hkv * ((long long)a.rows.max_rows * G / 16 + 1) * rows->B < (1ll << 31) &&
+          (long long)rows->rows * hq < (1ll << 31),
+      "too many rows and heads for one launch");
+  if (ns > 1) {
+    if (!workspace || workspace_bytes <
+        ks_paged_attention_workspace_bytes(cache, rows->B, rows->rows, hq, rows->max_rows, len)) {
+      set_error("workspace smaller than ks_paged_attention_workspace_bytes");
+      return KS_ENOMEM;
+    }
+    REQ(((uintptr_t)workspace & 15) == 0, "workspace must be 16-byte aligned");
+  }
+  a.q = q;
+  a.out = out;
+  a.lse = lse;
+  a.ldq = ldq;
+  a.ldo = ldo;
+  a.hq = hq;
+  a.dtype = dtype;
+  a.scale = scale;
+  a.nsplit = a.nsplit_ld = ns;
+  a.span = ((len + ns - 1) / ns + 63) / 64 * 64;
+  a.part = ns > 1 ? (float*)workspace : nullptr;
+  ks::paged_attention(a, (hipStream_t)stream);
+  HIPCHK(hipGetLastError());
+  return KS_OK;
+}
+
 ks_status ks_hidden_cos(const float* X, const float* Y, int groups, int r, int d, float* out,
                         void* stream) {
   REQ(X && Y && out, "null pointer");

@@ -214,6 +214,65 @@ void attn_combine(const AttnArgs& a, const float* kvself, Act act_out, hipStream
 int attn_nsplit(int n_positions, int tiles);
 int attn_rows_per_block(int G, bool batched);
 
+// ------------------------------------------------------------ paged cache
+// One layer's pages (see ks_paged_cache) and the rows of a call over them.
+struct PagedCache {
+  void* k;
+  void* v;
+  float* k_scale;
+  float* v_scale;
+  int n_pages, page, lpage;  // lpage = log2(page)
+  int block, lblock;
+  int hkv, hd, kind;
+};
+struct PagedRows {
+  int B, rows;
+  const int32_t* row_start;  // device [B + 1]; nullptr: one sequence of all rows
+  const int32_t* pos0;       // device [B]
+  const int32_t* table;      // device [B][table_ld]
+  int table_ld;
+  int max_rows;  // of a sequence
+  int max_len;   // positions used, at most table_ld * page
+  int32_t* err;  // device [B] or nullptr
+};
+// q_out = rotated q and the rotated k and v stored at the rows' positions.  Internal
+// callers also have the heads normalised (gains) and read in the ks_pack_qkv order.
+struct PagedAppend {
+  PagedCache cache;
+  PagedRows rows;
+  const void* q;  // nullptr: keys and values only
+  const void* k;
+  const void* v;
+  void* q_out;
+  size_t ldq, ldk, ldv, ldqo;  // elements per row
+  int hq, dtype;
+  const float* rope;  // [rope_rows][hd/2][2] or nullptr
+  int rope_rows;
+  const float* q_gain = nullptr;
+  const float* k_gain = nullptr;
+  float eps = 0.f;
+  int perm = 0;
+};
+void paged_append(const PagedAppend& a, hipStream_t st);
+// Row i of sequence b attends positions [0, pos0[b] + i], or [0, len[row]).
+struct PagedAttn {
+  PagedCache cache;
+  PagedRows rows;
+  const void* q;
+  void* out;  // nullptr: only the partials are written
+  float* lse;
+  size_t ldq, ldo;
+  int hq, dtype;
+  float scale;
+  const int32_t* len;  // device [rows] or nullptr
+  float* part;         // [rows][hq][nsplit_ld][hd + 2], nullptr: one split
+  int nsplit, nsplit_ld, span;
+  int col_max = 0, cblocks = 0;  // set by paged_attention
+};
+void paged_attention(const PagedAttn& a, hipStream_t st);
+// splits of a launch over at most max_rows rows a sequence and max_len positions
+int paged_splits(int B, int hkv, int G, int max_rows, int max_len);
+
 // ---------------------------------------------------- vocabulary reductions
 // argmax (lowest index on ties) and top-1 probability of each of M rows of V
 // logits (rows ld floats apart); ws: argmax_ws_bytes(M, V) device bytes

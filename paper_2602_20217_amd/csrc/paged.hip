@@ -1,0 +1,826 @@
+// Paged cache of keys and values: the append of new rows (with the rotation of
+// queries and keys) and causal attention of ragged rows over it.
+//
+// A cache holds pages of `page` tokens, every kv head apart, in bf16 or in 8-bit
+// floating point (e4m3: 4 exponent and 3 mantissa bits, largest value 448) with
+// one float32 scale, a power of two, per `block` tokens and head:
+//
+//   keys    [n_pages][hkv][page][hd]            token-major
+//   values  [n_pages][hkv][page / 16][hd][16]   dimension-major in granules of 16 tokens
+//   scales  [n_pages][hkv][page / block]
+//
+// Both layouts are what the matrix instructions of the attention take: a 16x16x32
+// product reads 8 consecutive contraction elements per lane, which are dimensions
+// of one key in S = K Q^T and tokens of one dimension in O^T = V^T P^T, so keys and
+// values go from memory to operand registers with 16-byte loads and no transpose.
+//
+// A power of two as scale costs e4m3 nothing (its relative step does not depend on
+// the scale) and makes every change of scale exact but for codes that reach the
+// subnormal range, so earlier tokens of a block survive a later, larger token.
+//
+//  k_pg_append  new rows: rotation, scales, codes, and the rotated queries
+//  k_pg_dec     attention of few rows a sequence, split over the context
+//  k_pg_merge   joins the splits of a row
+#include "ks_internal.h"
+
+#include <algorithm>
+#include <cfloat>
+
+namespace ks {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int GRAN = 16;     // tokens of a value granule
+constexpr int E_MIN = -100;  // smallest scale: 2^E_MIN
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------------- 8 bits
+// Smallest power of two s with amax <= 448 s, at least 2^E_MIN: 448 = 1.75 2^8, so
+// the exponent of amax decides, and whether its mantissa lies above 1.75.
+__device__ inline float scale_for(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  int e = (int)(u >> 23) - 127 - 8 + ((u & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  e = max(e, E_MIN);
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+// 1 / s of a power of two in [2^-126, 2^126]
+__device__ inline float inv_pow2(float s) {
+  return __uint_as_float((254u << 23) - (__float_as_uint(s) & 0x7F800000u));
+}
+__device__ inline bool finite_f(float x) { return fabsf(x) <= FLT_MAX; }
+// nearest code (ties to even) of a finite |x| <= 448; what is not finite becomes NaN
+__device__ inline uint32_t code_of(float x) {
+  const uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, 0.f, 0, false) & 0xFFu;
+  return finite_f(x) ? c : 0x7Fu;
+}
+__device__ inline float value_of(uint32_t code) {
+  return __builtin_amdgcn_cvt_f32_fp8((int)code, 0);
+}
+
+__device__ inline float ld1(const float* p) { return *p; }
+__device__ inline float ld1(const bf16_t* p) { return bf2f(*p); }
+__device__ inline void st1(float* p, float x) { *p = x; }
+__device__ inline void st1(bf16_t* p, float x) { *p = f2bf(x); }
+
+template <int N>  // sum over aligned groups of N lanes
+__device__ inline float group_sum(float v) {
+#pragma unroll
+  for (int o = N / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+__device__ inline float wave_max64(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  return v;
+}
+
+// Rows of sequence b, as far as the call's tensors and bounds hold them.
+struct SeqRows {
+  int r0, n;
+  bool over;  // it has more rows than max_rows
+};
+__device__ inline SeqRows seq_rows(const PagedRows& s, int b) {
+  if (!s.row_start) return SeqRows{0, s.rows, false};
+  const int a = min(max(s.row_start[b], 0), s.rows);
+  const int e = min(max(s.row_start[b + 1], a), s.rows);
+  return SeqRows{a, min(e - a, s.max_rows), e - a > s.max_rows};
+}
+
+// Position of sequence b's first row; far outside any cache it stands for the same
+// as here, with room to add a row number.
+__device__ inline int first_pos(const PagedRows& s, int b) {
+  return min(max(s.pos0[b], -(1 << 30)), 1 << 30);
+}
+// Positions that a row attends, in [0, max_len]; over: there are more.
+__device__ inline int row_len(const PagedAttn& a, const SeqRows& sr, int b, int r, bool& over) {
+  const int n = a.len ? a.len[sr.r0 + r] : first_pos(a.rows, b) + r + 1;
+  over |= n > a.rows.max_len;
+  return min(max(n, 0), a.rows.max_len);
+}
+
+// Sequence of row r: the last b with row_start[b] <= r, 64 boundaries a step; -1
+// for a row behind the last sequence.  Wave-uniform r.
+__device__ inline int seq_of(const PagedRows& s, int r) {
+  if (!s.row_start) return r < s.rows ? 0 : -1;
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 1; b0 <= s.B; b0 += 64) {
+    const int b = b0 + lane;
+    const uint64_t past = __ballot(b <= s.B && s.row_start[min(b, s.B)] > r);
+    if (past) return b0 - 1 + __ffsll((unsigned long long)past) - 1;
+  }
+  return -1;
+}
+
+// ------------------------------------------------------------------- append
+// Rotation of the pair (f, f + hd/2) of a head by the table's angle of its
+// position, after an optional RMS norm over the head (gain != nullptr).
+// LT = hd/2 lanes hold one row, lane f its pair.
+template <int LT>
+__device__ inline float2 turn(float x0, float x1, const float* cs, const float* gain, float eps,
+                              int f) {
+  if (gain) {
+    const float ss = group_sum<LT>(x0 * x0 + x1 * x1);
+    const float r = 1.0f / sqrtf(ss / (float)(2 * LT) + eps);
+    x0 = x0 * r * gain[f];
+    x1 = x1 * r * gain[f + LT];
+  }
+  if (!cs) return make_float2(x0, x1);
+  const float2 c = *(const float2*)(cs + 2 * f);
+  return make_float2(x0 * c.x - x1 * c.y, x1 * c.x + x0 * c.y);
+}
+
+// Workgroups [0, n_kv): one scale block (bf16: 16 tokens) of one head of one
+// sequence each; waves 0 and 1 take its keys, 2 and 3 its values.  A workgroup
+// owns all codes of its block, so it may change the block's scale.  Workgroups
+// from n_kv on: one row and query head per wave.
+template <typename T, int HD, bool E4>
+__global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int touched) {
+  constexpr int LT = HD / 2;   // lanes of a key or query row
+  constexpr int TP = 64 / LT;  // rows a wave holds at a time
+  const PagedCache& c = a.cache;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int f = lane % LT, sub = lane / LT;
+  const int c0 = a.perm ? qkv_perm(f, HD) : f, c1 = a.perm ? qkv_perm(f + LT, HD) : f + LT;
+
+  if ((int)blockIdx.x >= n_kv) {
+    const int job = ((int)blockIdx.x - n_kv) * 4 + wave;
+    const int r = job / ((a.hq + TP - 1) / TP);
+    const int h = job % ((a.hq + TP - 1) / TP) * TP + sub;
+    if (r >= a.rows.rows) return;
+    const int b = seq_of(a.rows, r);
+    if (b < 0) return;
+    const SeqRows sr = seq_rows(a.rows, b);
+    if (r - sr.r0 >= sr.n) return;
+    const int p = first_pos(a.rows, b) + (r - sr.r0);
+    const bool ok = p >= 0 && (!a.rope || p < a.rope_rows);
+    const T* src = (const T*)a.q + (size_t)r * a.ldq + (size_t)min(h, a.hq - 1) * HD;
+    float2 y = turn<LT>(ld1(src + c0), ld1(src + c1),
+                        a.rope && ok ? a.rope + (size_t)p * HD : nullptr, a.q_gain, a.eps, f);
+    if (!ok) y = make_float2(0.f, 0.f);
+    if (h < a.hq) {
+      T* dst = (T*)a.q_out + (size_t)r * a.ldqo + (size_t)h * HD;
+      st1(dst + f, y.x);
+      st1(dst + f + LT, y.y);
+    }
+    return;
+  }
+
+  const int t = blockIdx.x % touched;
+  const int h = blockIdx.x / touched % c.hkv;
+  const int b = blockIdx.x / touched / c.hkv;
+  const SeqRows sr = seq_rows(a.rows, b);
+  const int p0 = first_pos(a.rows, b);
+  const int lblock = E4 ? c.lblock : 4, block = 1 << lblock;
+  // new tokens are [pa, pe); rows at negative positions are padding
+  const int pa = max(p0, 0);
+  const int cap = min(a.rope ? a.rope_rows : INT32_MAX, a.rows.max_len);
+  const int pe = min(p0 + sr.n, cap);
+  if (a.rows.err && t == 0 && threadIdx.x == 0 && (sr.over || p0 + sr.n > cap)) a.rows.err[b] = 1;
+  const long long bs_ = ((long long)(pa >> lblock) + t) << lblock;  // first token of the block
+  if (bs_ >= pe) return;
+  const int bs = (int)bs_;
+  const int n0 = max(bs, pa), n1 = min(bs + block, pe);  // its new tokens
+  if (n0 >= n1) return;
+  const int pid = a.rows.table[(size_t)b * a.rows.table_ld + (bs >> c.lpage)];
+  if (pid < 0 || pid >= c.n_pages) {
+    if (a.rows.err && threadIdx.x == 0) a.rows.err[b] = 1;
+    return;
+  }
+  const int s0 = bs & (c.page - 1);  // the block's first slot in its page
+  const size_t head = (size_t)pid * c.hkv + h;
+  const bool is_k = wave < 2;
+  const int row_of = sr.r0 - p0;  // row of position p: row_of + p
+  const T* src = (const T*)(is_k ? a.k : a.v) + (size_t)h * HD;
+  const size_t ld = is_k ? a.ldk : a.ldv;
+
+  float s = 1.f, inv = 1.f, ratio = 1.f;
+  if (E4) {
+    __shared__ float s_max[4];
+    float* sp = (is_k ? c.k_scale : c.v_scale) + (head << (c.lpage - lblock)) + (s0 >> lblock);
+    const float s_old = n0 > bs ? *sp : 0.f;  // earlier tokens only
+    float amax = 0.f;
+    if (is_k) {
+      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
+        const int pp = min(p, n1 - 1);
+        const T* x = src + (size_t)(row_of + pp) * ld;
+        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
+                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
+        if (finite_f(y.x)) amax = fmaxf(amax, fabsf(y.x));
+        if (finite_f(y.y)) amax = fmaxf(amax, fabsf(y.y));
+      }
+    } else if ((int)threadIdx.x - 128 < HD) {
+      for (int p = n0; p < n1; ++p) {
+        const float y = ld1(src + (size_t)(row_of + p) * ld + (threadIdx.x - 128));
+        if (finite_f(y)) amax = fmaxf(amax, fabsf(y));
+      }
+    }
+    amax = wave_max64(amax);
+    if (lane == 0) s_max[wave] = amax;
+    __syncthreads();
+    s = fmaxf(s_old, scale_for(is_k ? fmaxf(s_max[0], s_max[1]) : fmaxf(s_max[2], s_max[3])));
+    inv = inv_pow2(s);
+    ratio = s_old * inv;  // earlier codes are multiplied by it
+    if ((threadIdx.x & 127) == 0) *sp = s;
+  }
+
+  if (is_k) {
+    const size_t base = (head << c.lpage) * HD + (size_t)s0 * HD;
+    if (E4) {
+      uint8_t* kc = (uint8_t*)c.k + base;
+      if (n0 > bs && ratio != 1.f)
+        for (int i = wave * 64 + lane; i < (n0 - bs) * HD; i += 128)
+          kc[i] = (uint8_t)code_of(value_of(kc[i]) * ratio);
+      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
+        const int pp = min(p, n1 - 1);
+        const T* x = src + (size_t)(row_of + pp) * ld;
+        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
+                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
+        if (p < n1) {
+          uint8_t* dst = kc + (size_t)(p - bs) * HD;
+          dst[f] = (uint8_t)code_of(y.x * inv);
+          dst[f + LT] = (uint8_t)code_of(y.y * inv);
+        }
+      }
+    } else {
+      bf16_t* kc = (bf16_t*)c.k + base;
+      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
+        const int pp = min(p, n1 - 1);
+        const T* x = src + (size_t)(row_of + pp) * ld;
+        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
+                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
+        if (p < n1) {
+          bf16_t* dst = kc + (size_t)(p - bs) * HD;
+          dst[f] = f2bf(y.x);
+          dst[f + LT] = f2bf(y.y);
+        }
+      }
+    }
+    return;
+  }
+  const int d = threadIdx.x - 128;
+  if (d >= HD) return;
+  for (int g0 = bs; g0 < n1; g0 += GRAN) {  // granules that the block's tokens reach
+    if (g0 + GRAN <= n0 && (!E4 || ratio == 1.f)) continue;
+    const size_t off = ((head << c.lpage) + (size_t)(s0 + g0 - bs)) * HD + (size_t)d * GRAN;
+    if (E4) {
+      uint8_t* vc = (uint8_t*)c.v + off;
+      uint32_t w[4];
+      *(uint4*)w = *(const uint4*)vc;
+#pragma unroll
+      for (int i = 0; i < GRAN; ++i) {
+        const int p = g0 + i;
+        uint32_t cd = (w[i / 4] >> (8 * (i % 4))) & 0xFFu;
+        if (p < n0) {
+          if (ratio != 1.f) cd = code_of(value_of(cd) * ratio);
+        } else if (p < n1) {
+          cd = code_of(ld1(src + (size_t)(row_of + p) * ld + d) * inv);
+        }
+        w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
+      }
+      *(uint4*)vc = *(const uint4*)w;
+    } else {
+      bf16_t* vc = (bf16_t*)c.v + off;
+      for (int i = 0; i < GRAN; ++i) {
+        const int p = g0 + i;
+        if (p >= n0 && p < n1) vc[i] = f2bf(ld1(src + (size_t)(row_of + p) * ld + d));
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------- attention
+constexpr int DEC_NW = 4;       // waves of a split workgroup
+constexpr int KT = 64;          // keys of a tile
+constexpr int SPAN_MAX = 16384; // positions of a split (its page ids lie in LDS)
+
+// One wave's operand registers of a tile: 64 keys, 64 values.  Key row i of
+// subtile kt is key 16 (i / 4) + 4 kt + i % 4 of the tile, so lane group g of the
+// score registers holds the 16 consecutive keys from 16 g: one granule of values.
+//  keys    lane (i, g), i = lane % 16: row i of each subtile.  e4m3: 16 dims
+//          from 64 j + 16 g; bf16: 8 dims from 32 j + 8 g
+//  values  lane (i, g): dim 16 db + i, tokens 16 g..16 g + 15
+template <int HD, bool E4>
+struct Tile {
+  static constexpr int KJ = E4 ? HD / 64 : HD / 32;
+  static constexpr int VJ = E4 ? 1 : 2;
+  u32x4 k[4][KJ];
+  u32x4 v[HD / 16][VJ];
+};
+
+// 8 codes of two words as bf16, times the scale (exact)
+__device__ inline bf16x8 widen(uint32_t w0, uint32_t w1, float s) {
+  const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w0, s, false);
+  const bf16x2_t b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w0, s, true);
+  const bf16x2_t c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w1, s, false);
+  const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)w1, s, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Dimension of element e of contraction step s, lane group g: the order in which
+// the key loads deliver them.
+template <bool E4>
+__device__ inline int dim_of(int s, int g) {
+  return E4 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+}
+
+// 8 query elements as QP bf16 planes that add up to them: one plane holds bf16
+// queries exactly, three hold float32 ones to 24 bits
+template <int QP>
+__device__ inline void load_q(const void* p, bool f32, bf16x8 (&o)[QP]) {
+  if (QP == 1) {
+    o[0] = __builtin_bit_cast(bf16x8, *(const u32x4*)p);
+    return;
+  }
+  const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
+  const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float r = x[e];
+#pragma unroll
+    for (int n = 0; n < QP; ++n) {
+      o[n][e] = (__bf16)r;
+      r -= (float)o[n][e];
+    }
+  }
+}
+
+__device__ inline uint32_t bytes_below(int n) {  // mask of the first n of 4 bytes
+  return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+}
+
+// Few rows.  A workgroup of four waves owns one split of `span` positions of one
+// kv head of one sequence and 16 CB of its query columns (column c: row c / G,
+// query head c % G of the kv head); wave w takes the split's tiles w, w + 4, ...
+// and runs a softmax with a running maximum and sum over them.  Keys are
+// requested again as soon as the scores are computed and values as soon as they
+// are added, so a tile's loads are in flight during the arithmetic of the one
+// before.  The four results meet in LDS, in wave order.
+//
+// A column's arithmetic depends on its own query and length and on the split
+// only, never on the other columns or on CB.
+//
+// Masked places: a key past a column's length is masked in the scores, whatever
+// it holds; a value there meets probability 0, so it must not be infinite or
+// NaN: values past the longest length are zeroed, and where those between the
+// shortest and the longest length hold one, the rows are added one at a time.
+template <int HD, bool E4, int QP, int CB>
+__global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
+  constexpr int PP = QP;               // probability planes, as of the queries
+  constexpr int NS = HD / 32;          // contraction steps of a score
+  constexpr int ND = HD / 16;          // blocks of 16 output dims
+  constexpr int RS = HD + 4;           // LDS merge record per column (bank-shifted)
+  typedef Tile<HD, E4> TileT;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const PagedCache& c = a.cache;
+  const int G = a.hq / c.hkv;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i16 = lane & 15, g = lane >> 4;
+
+  int id = blockIdx.x;
+  const int split = id % a.nsplit;
+  id /= a.nsplit;
+  const int kvh = id % c.hkv;
+  id /= c.hkv;
+  const int col0 = id % a.cblocks * 16 * CB;
+  const int b = id / a.cblocks;
+  const SeqRows sr = seq_rows(a.rows, b);
+  if (a.rows.err && threadIdx.x == 0 && sr.over) a.rows.err[b] = 1;
+  const int ncol = min(sr.n * G - col0, 16 * CB);
+  if (ncol <= 0) return;
+  if (sr.n * G > a.col_max) return;  // a sequence of the chunk kernel
+
+  // lengths: of this lane's columns, and the shortest and longest of the block
+  int len[CB], lmin = INT32_MAX, lmax = 0;
+  bool over = false;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int cc = 16 * cb + i16;
+    const int r = (col0 + min(cc, ncol - 1)) / G;
+    len[cb] = row_len(a, sr, b, r, over);
+    lmin = min(lmin, len[cb]);
+    lmax = max(lmax, len[cb]);
+  }
+#pragma unroll
+  for (int o = 8; o >= 1; o >>= 1) {
+    lmin = min(lmin, __shfl_xor(lmin, o));
+    lmax = max(lmax, __shfl_xor(lmax, o));
+  }
+  lmin = __builtin_amdgcn_readfirstlane(lmin);
+  lmax = __builtin_amdgcn_readfirstlane(lmax);
+  if (a.rows.err && over) a.rows.err[b] = 1;
+  const int start = split * a.span;
+  const int stop = min(lmax, start + a.span);
+  if (start >= stop && split > 0) return;  // no partial is read from here
+
+  // the split's page ids
+  int* s_page = (int*)smem;
+  const int np = stop > start ? ((stop - 1) >> c.lpage) - (start >> c.lpage) + 1 : 0;
+  for (int i = threadIdx.x; i < np; i += 64 * DEC_NW) {
+    const int pid = a.rows.table[(size_t)b * a.rows.table_ld + (start >> c.lpage) + i];
+    const bool ok = pid >= 0 && pid < c.n_pages;
+    s_page[i] = ok ? pid : -1;
+    if (!ok && a.rows.err) a.rows.err[b] = 1;
+  }
+
+  // query columns
+  bf16x8 q[CB][NS][QP];
+  const size_t es = QP == 1 ? 2 : 4;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    const int cc = col0 + min(16 * cb + i16, ncol - 1);
+    const char* p = (const char*)a.q +
+                    ((size_t)(sr.r0 + cc / G) * a.ldq + (size_t)(kvh * G + cc % G) * HD) * es;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) load_q<QP>(p + dim_of<E4>(s, g) * es, QP != 1, q[cb][s]);
+  }
+  __syncthreads();
+
+  f32x4 o[CB][ND];
+  float m[CB], l[CB];
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    m[cb] = -FLT_MAX;
+    l[cb] = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) o[cb][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  // granule gr of the tile at t0: its page's first token of this head, or -1
+  auto granule = [&](int t0, int gr) -> long long {
+    const int p = t0 + GRAN * gr;
+    if (p >= stop) return -1;
+    const int pid = s_page[(p >> c.lpage) - (start >> c.lpage)];
+    if (pid < 0) return -1;
+    return (((long long)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1));
+  };
+  const size_t eb = E4 ? 1 : 2;
+  auto load_k = [&](TileT& t, float& ks, int t0) {
+    const long long tok = max(granule(t0, i16 >> 2), 0ll);
+    const char* p = (const char*)c.k + ((size_t)tok + (i16 & 3)) * HD * eb + 16 * g;
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+      for (int j = 0; j < TileT::KJ; ++j)
+        t.k[kt][j] = *(const u32x4*)(p + (size_t)(4 * kt) * HD * eb + 64 * j);
+    if (E4) ks = c.k_scale[(size_t)(tok >> c.lblock)];
+  };
+  auto load_v = [&](TileT& t, float& vs, int t0) {
+    const long long tok = granule(t0, g);
+    const char* p = (const char*)c.v + ((size_t)max(tok, 0ll) * HD + (size_t)i16 * GRAN) * eb;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int j = 0; j < TileT::VJ; ++j)
+        t.v[d][j] = *(const u32x4*)(p + (size_t)(16 * d) * GRAN * eb + 16 * j);
+    if (E4) vs = tok < 0 ? 1.f : c.v_scale[(size_t)(tok >> c.lblock)];
+  };
+
+  const float sc = a.scale * LOG2E;
+  TileT t;
+  float ks = 1.f, vs = 1.f;
+  int t0 = start + w * KT;
+  if (t0 < stop) {
+    load_k(t, ks, t0);
+    load_v(t, vs, t0);
+  }
+  for (; t0 < stop; t0 += DEC_NW * KT) {
+    const int tn = t0 + DEC_NW * KT;
+    // scores: row 4 g + v of subtile kt is key 16 g + 4 kt + v, column lane % 16
+    f32x4 s[CB][4];
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb) s[cb][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int st = 0; st < NS; ++st) {
+        bf16x8 kk;
+        if (E4) {
+          const u32x4 x = t.k[kt][st >> 1];
+          kk = (st & 1) ? widen(x[2], x[3], ks) : widen(x[0], x[1], ks);
+        } else {
+          kk = __builtin_bit_cast(bf16x8, t.k[kt][st]);
+        }
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int n = 0; n < QP; ++n)
+            s[cb][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, q[cb][st][n], s[cb][kt], 0, 0, 0);
+      }
+    }
+    const bool have = granule(t0, g) >= 0;  // this lane group's keys
+    float ksn = 1.f, vsn = 1.f;
+    if (tn < stop) load_k(t, ksn, tn);
+
+    // softmax step
+    const bool ragged = t0 + KT > lmin || __any(!have);
+    bf16x8 p[CB][2][PP];
+#pragma unroll
+    for (int cb = 0; cb < CB; ++cb) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          float x = s[cb][kt][v] * sc;
+          if (ragged && !(have && t0 + 16 * g + 4 * kt + v < len[cb])) x = -INFINITY;
+          s[cb][kt][v] = x;
+          mx = fmaxf(mx, x);
+        }
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mn = fmaxf(m[cb], mx);
+      const float al = __builtin_amdgcn_exp2f(m[cb] - mn);
+      m[cb] = mn;
+      float sum = 0.f;
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          const float e = __builtin_amdgcn_exp2f(s[cb][kt][v] - mn);
+          sum += e;
+          // one plane (bf16 rows) holds a probability to 2^-8, as the output is held;
+          // three (float32 rows) to 2^-24 (two, 2^-16, lose digits of the output)
+          float r = e;
+#pragma unroll
+          for (int n = 0; n < PP; ++n) {
+            p[cb][kt >> 1][n][4 * (kt & 1) + v] = (__bf16)r;
+            r -= (float)p[cb][kt >> 1][n][4 * (kt & 1) + v];
+          }
+        }
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      l[cb] = l[cb] * al + sum;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[cb][d] *= al;
+    }
+
+    // values
+    bool slow = false;
+    if (ragged) {
+      // this lane group's tokens below the longest and below the shortest length
+      const int hi = have ? min(lmax - (t0 + GRAN * g), GRAN) : 0;
+      const int lo = have ? min(lmin - (t0 + GRAN * g), GRAN) : 0;
+      uint32_t odd = 0;  // an infinite or NaN value between the two
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int j = 0; j < TileT::VJ; ++j)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            if (E4) {
+              const uint32_t in = bytes_below(hi - 4 * x);
+              const uint32_t y = t.v[d][j][x] & in;
+              t.v[d][j][x] = y;
+              odd |= ((y & 0x7F7F7F7Fu & ~bytes_below(lo - 4 * x)) + 0x01010101u) & 0x80808080u;
+            } else {
+              const int at = 8 * j + 2 * x;
+              const uint32_t in = bytes_below(2 * (hi - at));
+              const uint32_t y = t.v[d][j][x] & in;
+              t.v[d][j][x] = y;
+              const uint32_t z = y & 0x7FFF7FFFu & ~bytes_below(2 * (lo - at));
+              odd |= (z & 0xFFFFu) >= 0x7F80u || (z >> 16) >= 0x7F80u;
+            }
+          }
+      slow = __any(odd != 0);
+    }
+    if (!slow) {
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          bf16x8 vv;
+          if (E4)
+            vv = st ? widen(t.v[d][0][2], t.v[d][0][3], vs) : widen(t.v[d][0][0], t.v[d][0][1], vs);
+          else
+            vv = __builtin_bit_cast(bf16x8, t.v[d][TileT::VJ == 2 ? st : 0]);
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+            for (int n = 0; n < PP; ++n)
+              o[cb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], o[cb][d], 0, 0, 0);
+        }
+    } else {
+      for (int r = col0 / G; r <= (col0 + ncol - 1) / G; ++r) {
+        // the row's own length, and its tokens of this lane group
+        const int rl = row_len(a, sr, b, r, over);
+        const int hi = have ? min(rl - (t0 + GRAN * g), GRAN) : 0;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          f32x4 add[CB];
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb) add[cb] = o[cb][d];
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            bf16x8 vv;
+            if (E4) {
+              const uint32_t w0 = t.v[d][0][2 * st] & bytes_below(hi - 8 * st);
+              const uint32_t w1 = t.v[d][0][2 * st + 1] & bytes_below(hi - 8 * st - 4);
+              vv = widen(w0, w1, vs);
+            } else {
+              u32x4 x = t.v[d][TileT::VJ == 2 ? st : 0];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) x[y] &= bytes_below(2 * (hi - 8 * st - 2 * y));
+              vv = __builtin_bit_cast(bf16x8, x);
+            }
+#pragma unroll
+            for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+              for (int n = 0; n < PP; ++n)
+                add[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], add[cb], 0, 0, 0);
+          }
+#pragma unroll
+          for (int cb = 0; cb < CB; ++cb)
+            if ((col0 + 16 * cb + i16) / G == r) o[cb][d] = add[cb];
+        }
+      }
+    }
+    if (tn < stop) load_v(t, vsn, tn);
+    ks = ksn;
+    vs = vsn;
+  }
+
+  // merge of the waves: record of wave w, column cc at (w 16 CB + cc) RS
+  __syncthreads();  // the page ids are no longer read
+  float* rec = (float*)smem;
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    float* x = rec + (size_t)(w * 16 * CB + 16 * cb + i16) * RS;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) *(f32x4*)(x + 16 * d + 4 * g) = o[cb][d];
+    if (g == 0) {
+      x[HD] = m[cb];
+      x[HD + 1] = l[cb];
+    }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < ncol * (HD / 4); e += 64 * DEC_NW) {
+    const int cc = e / (HD / 4), d = e % (HD / 4) * 4;
+    const int row = (col0 + cc) / G, h = kvh * G + (col0 + cc) % G;
+    const int n = row_len(a, sr, b, row, over);
+    if (n <= start && a.part) continue;  // not read by the merge
+    float mm = -FLT_MAX;
+#pragma unroll
+    for (int k = 0; k < DEC_NW; ++k) mm = fmaxf(mm, rec[(size_t)(k * 16 * CB + cc) * RS + HD]);
+    float ll = 0.f;
+    f32x4 oo{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < DEC_NW; ++k) {
+      const float* x = rec + (size_t)(k * 16 * CB + cc) * RS;
+      const float f = __builtin_amdgcn_exp2f(x[HD] - mm);
+      ll = fmaf(x[HD + 1], f, ll);
+      const f32x4 y = *(const f32x4*)(x + d);
+#pragma unroll
+      for (int v = 0; v < 4; ++v) oo[v] = fmaf(y[v], f, oo[v]);
+    }
+    const size_t r = sr.r0 + row;
+    if (a.part) {
+      float* x = a.part + ((r * a.hq + h) * a.nsplit_ld + split) * (HD + 2);
+      *(float2*)(x + d) = make_float2(oo[0], oo[1]);
+      *(float2*)(x + d + 2) = make_float2(oo[2], oo[3]);
+      if (d == 0) *(float2*)(x + HD) = make_float2(mm * LN2, ll);
+      continue;
+    }
+    const float inv = n > 0 ? 1.0f / ll : 0.f;
+    const size_t at = r * a.ldo + (size_t)h * HD + d;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+      const float y = n > 0 ? oo[v] * inv : 0.f;
+      if (QP == 1) ((bf16_t*)a.out)[at + v] = f2bf(y);
+      else ((float*)a.out)[at + v] = y;
+    }
+    if (d == 0 && a.lse) a.lse[r * a.hq + h] = n > 0 ? mm * LN2 + logf(ll) : -INFINITY;
+  }
+}
+
+// One wave per (row, query head): joins the splits that hold keys of the row, in
+// order.  Partials are (o[hd], max, sum) with the maximum in natural units.
+template <typename T, int HD>
+__global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
+  constexpr int DPL = HD / 64;
+  const int lane = threadIdx.x & 63;
+  const int job = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int r = job / a.hq, h = job % a.hq;
+  if (r >= a.rows.rows) return;
+  const int b = seq_of(a.rows, r);
+  if (b < 0) return;
+  const SeqRows sr = seq_rows(a.rows, b);
+  if (r - sr.r0 >= sr.n || sr.n * (a.hq / a.cache.hkv) > a.col_max) return;
+  bool over = false;
+  const int n = row_len(a, sr, b, r - sr.r0, over);
+  const int ns = (n + a.span - 1) / a.span;
+  const float* p = a.part + ((size_t)r * a.hq + h) * a.nsplit_ld * (HD + 2);
+  float m = -FLT_MAX, l = 0.f, o[DPL];
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) o[e] = 0.f;
+  constexpr int U = 8;
+  for (int s0 = 0; s0 < ns; s0 += U) {
+    float ms[U], ls[U], ov[U][DPL];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      ms[k] = -FLT_MAX;
+      ls[k] = 0.f;
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) ov[k][e] = 0.f;
+      if (s0 + k < ns) {
+        const float* x = p + (size_t)(s0 + k) * (HD + 2);
+        ms[k] = x[HD];
+        ls[k] = x[HD + 1];
+#pragma unroll
+        for (int e = 0; e < DPL; ++e) ov[k][e] = x[DPL * lane + e];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float mn = fmaxf(m, ms[k]);
+      const float ea = __expf(m - mn), eb = __expf(ms[k] - mn);
+      l = fmaf(ls[k], eb, l * ea);
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) o[e] = fmaf(ov[k][e], eb, o[e] * ea);
+      m = mn;
+    }
+  }
+  T* dst = (T*)a.out + (size_t)r * a.ldo + (size_t)h * HD + DPL * lane;
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) st1(dst + e, n > 0 ? o[e] * inv : 0.f);
+  if (lane == 0 && a.lse) a.lse[(size_t)r * a.hq + h] = n > 0 ? m + logf(l) : -INFINITY;
+}
+
+}  // namespace
+
+void paged_append(const PagedAppend& a, hipStream_t st) {
+  const PagedCache& c = a.cache;
+  const int block = c.kind == KS_E4M3 ? c.block : GRAN;
+  const int touched = (a.rows.max_rows + block - 2) / block + 1;
+  const int n_kv = a.rows.B * c.hkv * touched;
+  const int tp = 128 / c.hd;  // query heads of a wave
+  const int jobs = a.q ? a.rows.rows * ((a.hq + tp - 1) / tp) : 0;
+  const dim3 grid(n_kv + (jobs + 3) / 4);
+#define KS_APP(T_, HD_, E_) \
+  KS_LAUNCH((k_pg_append<T_, HD_, E_>), grid, dim3(256), 0, st, a, n_kv, touched)
+#define KS_APP_T(T_)                                                   \
+  do {                                                                 \
+    if (c.hd == 128 && c.kind == KS_E4M3) KS_APP(T_, 128, true);       \
+    else if (c.hd == 128) KS_APP(T_, 128, false);                      \
+    else if (c.kind == KS_E4M3) KS_APP(T_, 64, true);                  \
+    else KS_APP(T_, 64, false);                                        \
+  } while (0)
+  if (a.dtype == KS_BF16) KS_APP_T(bf16_t);
+  else KS_APP_T(float);
+#undef KS_APP_T
+#undef KS_APP
+}
+
+int paged_splits(int B, int hkv, int G, int max_rows, int max_len) {
+  const int blocks = B * hkv * ((max_rows * G + 31) / 32);
+  const int most = std::max(1, (max_len + DEC_NW * KT - 1) / (DEC_NW * KT));
+  const int want = std::max((1024 + blocks - 1) / blocks, (max_len + SPAN_MAX - 1) / SPAN_MAX);
+  return std::min(want, most);
+}
+
+void paged_attention(const PagedAttn& a_, hipStream_t st) {
+  PagedAttn a = a_;
+  const PagedCache& c = a.cache;
+  const int G = a.hq / c.hkv;
+  a.col_max = INT32_MAX;
+  const int cols = a.rows.max_rows * G;
+  const int CB = cols <= 16 ? 1 : 2;
+  a.cblocks = (cols + 16 * CB - 1) / (16 * CB);
+  const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
+  const int np = a.span / c.page + 2;
+  const size_t lds = std::max((size_t)DEC_NW * 16 * CB * (c.hd + 4) * 4, (size_t)np * 4);
+#define KS_DEC(HD_, E_, QP_)                                                              \
+  do {                                                                                    \
+    if (CB == 1) KS_LAUNCH((k_pg_dec<HD_, E_, QP_, 1>), grid, dim3(256), lds, st, a);     \
+    else KS_LAUNCH((k_pg_dec<HD_, E_, QP_, 2>), grid, dim3(256), lds, st, a);             \
+  } while (0)
+#define KS_DEC_T(QP_)                                                  \
+  do {                                                                 \
+    if (c.hd == 128 && c.kind == KS_E4M3) KS_DEC(128, true, QP_);      \
+    else if (c.hd == 128) KS_DEC(128, false, QP_);                     \
+    else if (c.kind == KS_E4M3) KS_DEC(64, true, QP_);                 \
+    else KS_DEC(64, false, QP_);                                       \
+  } while (0)
+  if (a.dtype == KS_BF16) KS_DEC_T(1);
+  else KS_DEC_T(3);
+#undef KS_DEC_T
+#undef KS_DEC
+  if (!a.part || !a.out) return;
+  const dim3 mgrid((unsigned)(((size_t)a.rows.rows * a.hq + 3) / 4));
+#define KS_MRG(T_, HD_) KS_LAUNCH((k_pg_merge<T_, HD_>), mgrid, dim3(256), 0, st, a)
+  if (a.dtype == KS_BF16) {
+    if (c.hd == 128) KS_MRG(bf16_t, 128);
+    else KS_MRG(bf16_t, 64);
+  } else {
+    if (c.hd == 128) KS_MRG(float, 128);
+    else KS_MRG(float, 64);
+  }
+#undef KS_MRG
+}
+
+}  // namespace ks

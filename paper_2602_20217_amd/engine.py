@@ -396,3 +396,169 @@ def knapsack_batch_select(best, bits, w, s, C_cap: int, D: int = 10):
     K.ks_knapsack_batch_select(_ptr(best), _ptr(bits), _ptr(w), _ptr(s), B, n, C_cap, D, _ptr(js),
                                _ptr(gs), _ptr(tpt), _ptr(skip), _stream())
     return js, gs, tpt, skip
+
+
+# ------------------------------------------------------------ paged cache
+def _need(ok: bool, msg: str):
+    if not ok:
+        raise ValueError(msg)
+
+
+def _here(dev: torch.device, f, *args):
+    """Calls f with args and the current stream of dev, dev being current."""
+    if dev.index == torch.cuda.current_device():
+        f(*args, _stream())
+    else:
+        with torch.cuda.device(dev):
+            f(*args, _stream())
+
+
+_DT = {torch.float32: K.KS_F32, torch.bfloat16: K.KS_BF16}
+
+
+def _rows3(t: torch.Tensor, heads: int, hd: int, name: str) -> int:
+    """Row stride (elements) of t [rows, heads, hd], dense inside a row."""
+    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == hd and
+          (t.shape[0] == 0 or t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd)),
+          f"{name} must be [rows, {heads}, {hd}], dense rows")
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * hd)
+
+
+class PagedCache:
+    """One layer's pages of keys and values (see ks_paged_cache): kind "e4m3" (8-bit
+    floats, a scale for every `block` tokens and head) or "bf16".
+
+    k is [n_pages, hkv, page, hd], v [n_pages, hkv, page // 16, hd, 16], the scales
+    [n_pages, hkv, page // block] float32.  ``over`` wraps tensors of those shapes.
+    """
+
+    def __init__(self, n_pages: int, page: int, hkv: int, hd: int, kind: str = "e4m3",
+                 block: int = 16, device="cuda"):
+        _need(kind in ("e4m3", "bf16"), "kind must be 'e4m3' or 'bf16'")
+        _need(page >= 16 and page % 16 == 0, "page must be a multiple of 16")
+        dt = torch.float8_e4m3fn if kind == "e4m3" else torch.bfloat16
+        z = lambda dt, *s: torch.zeros(*s, dtype=dt, device=device)
+        self._set(z(dt, n_pages, hkv, page, hd), z(dt, n_pages, hkv, page // 16, hd, 16),
+                  *([z(torch.float32, n_pages, hkv, page // block) for _ in range(2)]
+                    if kind == "e4m3" else [None, None]))
+
+    @classmethod
+    def over(cls, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None,
+             v_scale: torch.Tensor | None = None) -> "PagedCache":
+        c = cls.__new__(cls)
+        c._set(k, v, k_scale, v_scale)
+        return c
+
+    def _set(self, k, v, k_scale, v_scale):
+        _need(k.dim() == 4 and k.dtype in (torch.bfloat16, torch.float8_e4m3fn, torch.uint8),
+              "k must be [n_pages, hkv, page, hd] of bfloat16, float8_e4m3fn or uint8")
+        n, hkv, page, hd = k.shape
+        _need(v.shape == (n, hkv, page // 16, hd, 16) and v.dtype == k.dtype,
+              "v must be [n_pages, hkv, page // 16, hd, 16] of k's type")
+        e4 = k.dtype != torch.bfloat16
+        block = 16
+        _need((k_scale is not None) == e4 and (v_scale is not None) == e4,
+              "8-bit caches have scales, bf16 ones none")
+        if e4:
+            nb = k_scale.shape[-1]
+            _need(nb >= 1 and page % nb == 0, "a page holds a whole number of blocks")
+            block = page // nb
+            for s in (k_scale, v_scale):
+                _need(s.shape == (n, hkv, nb) and s.dtype == torch.float32,
+                      "scales must be float32 [n_pages, hkv, page // block]")
+        ts = [t for t in (k, v, k_scale, v_scale) if t is not None]
+        _need(all(t.is_contiguous() and t.device == k.device for t in ts),
+              "cache tensors must be contiguous and on one device")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.device = k.device
+        self.page, self.block, self.hkv, self.hd = page, block, hkv, hd
+        self.desc = K.PagedCache(_ptr(k), _ptr(v), _ptr(k_scale) if e4 else None,
+                                 _ptr(v_scale) if e4 else None, n, page, block, hkv, hd,
+                                 K.KS_E4M3 if e4 else K.KS_BF16)
+        self.ref = C.byref(self.desc)
+
+
+def _paged_rows(cache: PagedCache, table, row_start, pos0, rows, max_rows, max_len, err):
+    B = pos0.shape[0]
+    i32 = torch.int32
+    _need(table.dim() == 2 and table.shape[0] == B and table.dtype == i32
+          and table.stride(1) == 1 and table.device == cache.device,
+          "table must be int32 [B, pages], dense rows, on the cache's device")
+    _need(row_start.shape == (B + 1,) and row_start.dtype == i32 and row_start.is_contiguous()
+          and pos0.dtype == i32 and pos0.is_contiguous() and pos0.device == cache.device
+          and row_start.device == cache.device,
+          "row_start must be int32 [B + 1] and pos0 int32 [B], on the cache's device")
+    if err is not None:
+        _need(err.shape == (B,) and err.dtype == i32 and err.is_contiguous()
+              and err.device == cache.device, "err must be int32 [B] on the cache's device")
+    width = table.shape[1]
+    most = width * cache.page
+    return K.PagedRows(B, rows, _ptr(row_start), _ptr(pos0), _ptr(table),
+                       table.stride(0) if B > 1 else width,
+                       rows if max_rows is None else max_rows,
+                       most if max_len is None else min(max_len, most),
+                       None if err is None else _ptr(err))
+
+
+def paged_append(cache: PagedCache, table, row_start, pos0, k, v, q=None, rope=None, q_out=None,
+                 max_rows=None, err=None):
+    """Stores the rows' keys (rotated by rope [positions, hd/2, 2]) and values and
+    returns the rotated queries (in q_out, by default a new tensor; None without q).
+    See ks_paged_append; row strides are free, so slices of a fused projection do."""
+    hkv, hd, rows = cache.hkv, cache.hd, k.shape[0]
+    ldk, ldv = _rows3(k, hkv, hd, "k"), _rows3(v, hkv, hd, "v")
+    _need(k.dtype in _DT and v.dtype == k.dtype and v.shape[0] == rows
+          and k.device == cache.device and v.device == cache.device,
+          "k and v must be float32 or bfloat16, of the same rows, on the cache's device")
+    hq = ldq = ldo = 0
+    if q is not None:
+        hq = q.shape[1]
+        ldq = _rows3(q, hq, hd, "q")
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ldo = _rows3(q_out, hq, hd, "q_out")
+        _need(q.dtype == k.dtype and q_out.dtype == k.dtype and q.shape[0] == rows
+              and q_out.shape[0] == rows and q.device == cache.device
+              and q_out.device == cache.device, "q and q_out must match k")
+    if rope is not None:
+        _need(rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2) and rope.dtype == torch.float32
+              and rope.is_contiguous() and rope.device == cache.device,
+              "rope must be float32 [positions, hd / 2, 2] on the cache's device")
+    r = _paged_rows(cache, table, row_start, pos0, rows, max_rows, None, err)
+    _here(cache.device, K.ks_paged_append, cache.ref, C.byref(r), None if q is None else _ptr(q),
+          ldq, _ptr(k), ldk, _ptr(v), ldv, None if q is None else _ptr(q_out), ldo, hq,
+          _DT[k.dtype], None if rope is None else _ptr(rope), 0 if rope is None else rope.shape[0])
+    return q_out if q is not None else None
+
+
+def paged_attention_workspace(cache: PagedCache, B: int, rows: int, hq: int, max_rows: int,
+                              max_len: int) -> torch.Tensor:
+    """Workspace of paged_attention calls with at most these bounds; calls that may run
+    at the same time (on other streams, in other captured graphs) need one each."""
+    n = K.ks_paged_attention_workspace_bytes(cache.ref, B, rows, hq, max_rows, max_len)
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=cache.device)
+
+
+def paged_attention(cache: PagedCache, table, row_start, pos0, q, scale: float | None = None,
+                    out=None, lse=None, max_rows=None, max_len=None, workspace=None, err=None):
+    """Causal attention of the rows q [rows, hq, hd] over their sequences' pages (see
+    ks_paged_attention).  max_rows and max_len bound the rows and positions of a
+    sequence; they default to what the shapes allow, and tight ones are faster."""
+    rows, hq = q.shape[0], q.shape[1]
+    ldq = _rows3(q, hq, cache.hd, "q")
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    ldo = _rows3(out, hq, cache.hd, "out")
+    _need(q.dtype in _DT and out.dtype == q.dtype and out.shape[0] == rows
+          and q.device == cache.device and out.device == cache.device,
+          "q and out must be float32 or bfloat16, of the same rows, on the cache's device")
+    if lse is not None:
+        _need(lse.shape == (rows, hq) and lse.dtype == torch.float32 and lse.is_contiguous()
+              and lse.device == cache.device, "lse must be float32 [rows, hq]")
+    r = _paged_rows(cache, table, row_start, pos0, rows, max_rows, max_len, err)
+    if workspace is None:
+        workspace = paged_attention_workspace(cache, r.B, rows, hq, r.max_rows, r.max_len)
+    _here(cache.device, K.ks_paged_attention, cache.ref, C.byref(r), _ptr(q), ldq, _ptr(out), ldo,
+          hq, _DT[q.dtype], cache.hd ** -0.5 if scale is None else scale,
+          None if lse is None else _ptr(lse), _ptr(workspace), workspace.numel())
+    return out
