@@ -437,6 +437,42 @@ ks_status ks_spec_accept(const int32_t* p_ids, const float* p_probs, const int32
 ks_status ks_sample_uniforms(uint64_t seed, const int32_t* pos, int n, int purpose, float* out,
                              void* stream);
 
+/*
+ * ks_sample_draw: one token per logits row from a given uniform, every row with its
+ * own settings.  Entries are taken in the order of decreasing logit, equal ones by
+ * lower id, and pass, in turn: top_k (the first k; k <= 0 or >= the row's entries:
+ * off), the softmax of logit / temperature, min_p (probability at least min_p times
+ * the largest; <= 0: off, > 1 counts as 1) and top_p (the shortest prefix whose
+ * share of what is left reaches top_p; >= 1: off, <= 0: the first entry).  The token
+ * is the first entry whose cumulative share of what is kept exceeds u[row] (u below
+ * 0 or NaN counts as 0, u >= 1 takes the last one kept that has any mass).
+ * temperature <= 0 or NaN: the first entry in order (greedy).
+ * -inf and NaN logits are barred: never kept; a row without any other gets token -1,
+ * logprob -inf and kept 0.  +inf ties with +inf and leaves all others no mass.
+ * Shares are sums of integers in units of 2^-44 of the largest entry's, from
+ * exponentials in 64 bits: calls with the same inputs give the same tokens.  Unlike
+ * ks_sample_filter's, k may be as large as the vocabulary and nothing is tabulated.
+ * logits: device, dtype KS_F32 or KS_BF16, row r at logits + r * ld; 1 <= vocab <=
+ * 524288; rows <= 65535.  p: device arrays of rows values, of which temperature,
+ * top_k, top_p and min_p may be NULL (1 and off).  tokens (device int32[rows]);
+ * optional logprob (device float32[rows], log of the token's share of what was kept)
+ * and kept (device int32[rows], entries kept).  workspace: device,
+ * ks_sample_draw_workspace_bytes() bytes, 8-byte aligned; nothing in it needs to
+ * start at any value, and calls (or captured graphs) that may run at the same time
+ * need one each.  Asynchronous on stream.
+ */
+typedef struct ks_draw_params {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+} ks_draw_params;
+size_t ks_sample_draw_workspace_bytes(int rows, int vocab);
+ks_status ks_sample_draw(const void* logits, int dtype, int rows, int vocab, size_t ld,
+                         const ks_draw_params* p, int32_t* tokens, float* logprob, int32_t* kept,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- paged cache ---------------------------------------------------------- */
 /*
  * One layer's cache of keys and values in pages, shared by many sequences.  All

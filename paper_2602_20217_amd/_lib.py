@@ -77,6 +77,11 @@ class Sampling(C.Structure):
                 ("seed", C.c_uint64)]
 
 
+class DrawParams(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p),
+                ("min_p", C.c_void_p), ("u", C.c_void_p)]
+
+
 class PagedCache(C.Structure):
     _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
                 ("v_scale", C.c_void_p), ("n_pages", C.c_int), ("page", C.c_int),
@@ -157,6 +162,9 @@ _SIG = {
                                       _P, _P, _P]),
     "ks_spec_accept": (_I, [_P, _P, _P, _P, _P, _P, _P, _I, C.c_uint64, _I, _P, _P]),
     "ks_sample_uniforms": (_I, [C.c_uint64, _P, _I, _I, _P, _P]),
+    "ks_sample_draw_workspace_bytes": (C.c_size_t, [_I, _I]),
+    "ks_sample_draw": (_I, [_P, _I, _I, _I, C.c_size_t, C.POINTER(DrawParams), _P, _P, _P, _P,
+                            C.c_size_t, _P]),
     "ks_paged_append": (_I, [C.POINTER(PagedCache), C.POINTER(PagedRows), _P, C.c_size_t, _P,
                              C.c_size_t, _P, C.c_size_t, _P, C.c_size_t, _I, _I, _P, _I, _P]),
     "ks_paged_attention_workspace_bytes": (C.c_size_t, [C.POINTER(PagedCache), _I, _I, _I, _I,
@@ -222,6 +230,8 @@ ks_sample_filter_noalloc = _wrap("ks_sample_filter_noalloc")
 ks_spec_accept = _wrap("ks_spec_accept")
 ks_sample_uniforms = _wrap("ks_sample_uniforms")
 ks_sample_workspace_bytes = lib.ks_sample_workspace_bytes
+ks_sample_draw = _wrap("ks_sample_draw")
+ks_sample_draw_workspace_bytes = lib.ks_sample_draw_workspace_bytes
 ks_paged_append = _wrap("ks_paged_append")
 ks_paged_attention = _wrap("ks_paged_attention")
 ks_paged_attention_workspace_bytes = lib.ks_paged_attention_workspace_bytes

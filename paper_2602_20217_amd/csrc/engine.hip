@@ -1017,6 +1017,34 @@ ks_status ks_sample_uniforms(uint64_t seed, const int32_t* pos, int n, int purpo
   return KS_OK;
 }
 
+size_t ks_sample_draw_workspace_bytes(int rows, int vocab) {
+  if (rows < 0 || rows > 65535 || vocab < 1 || vocab > ks::DRAW_VOCAB_MAX) return 0;
+  return std::max<size_t>(ks::draw_ws_bytes(rows), 256);
+}
+
+ks_status ks_sample_draw(const void* logits, int dtype, int rows, int vocab, size_t ld,
+                         const ks_draw_params* p, int32_t* tokens, float* logprob, int32_t* kept,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  REQ(dtype == KS_F32 || dtype == KS_BF16, "dtype must be KS_F32 or KS_BF16");
+  REQ(rows >= 0 && rows <= 65535, "rows must be in [0, 65535]");
+  REQ(vocab >= 1 && vocab <= ks::DRAW_VOCAB_MAX, "vocab must be in [1, 524288]");
+  REQ(p, "null pointer");
+  if (rows == 0) return KS_OK;
+  REQ(logits && p->u && tokens && workspace, "null pointer");
+  REQ(ld >= (size_t)vocab, "ld must be at least vocab");
+  REQ(((uintptr_t)logits & (dtype == KS_BF16 ? 1 : 3)) == 0, "logits must be aligned to their type");
+  REQ(((uintptr_t)workspace & 7) == 0, "workspace must be 8-byte aligned");
+  if (workspace_bytes < ks_sample_draw_workspace_bytes(rows, vocab)) {
+    set_error("workspace smaller than ks_sample_draw_workspace_bytes");
+    return KS_ENOMEM;
+  }
+  ks::draw_rows(ks::DrawArgs{logits, dtype, rows, vocab, ld, p->temperature, p->top_k, p->top_p,
+                             p->min_p, p->u, tokens, logprob, kept, workspace},
+                (hipStream_t)stream);
+  HIPCHK(hipGetLastError());
+  return KS_OK;
+}
+
 static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
 
 static ks_status check_paged(const ks_paged_cache* c, const ks_paged_rows* r, ks::PagedCache& pc,

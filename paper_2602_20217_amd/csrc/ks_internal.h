@@ -307,6 +307,25 @@ void spec_accept(const int32_t* pid, const float* ppr, const int32_t* pcnt, cons
                  const float* qpr, const int32_t* qcnt, const int32_t* drafts, int g,
                  uint64_t seed, int pos0, int32_t* out, hipStream_t st);
 void uniforms(uint64_t seed, const int32_t* pos, int n, int purpose, float* out, hipStream_t st);
+// One token a row from a given uniform, settings by row (see ks_sample_draw; null
+// arrays: temperature 1, filters off).  ws: draw_ws_bytes(rows) device bytes.
+struct DrawArgs {
+  const void* logits;
+  int dtype, rows, vocab;
+  size_t ld;
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  const float* u;
+  int32_t* tokens;
+  float* logprob;
+  int32_t* kept;
+  void* ws;
+};
+constexpr int DRAW_VOCAB_MAX = 1 << 19;
+size_t draw_ws_bytes(int rows);
+void draw_rows(const DrawArgs& a, hipStream_t st);
 // out[g] = mean_t cos(X[g][t], Y[t])
 void cos_groups(const float* X, const float* Y, int groups, int r, int d, float* out,
                 hipStream_t st);

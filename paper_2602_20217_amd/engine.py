@@ -398,7 +398,7 @@ def knapsack_batch_select(best, bits, w, s, C_cap: int, D: int = 10):
     return js, gs, tpt, skip
 
 
-# ------------------------------------------------------------ paged cache
+# ------------------------------------------- draws and the paged cache
 def _need(ok: bool, msg: str):
     if not ok:
         raise ValueError(msg)
@@ -422,6 +422,40 @@ def _rows3(t: torch.Tensor, heads: int, hd: int, name: str) -> int:
           (t.shape[0] == 0 or t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd)),
           f"{name} must be [rows, {heads}, {hd}], dense rows")
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * hd)
+
+
+def sample_draw_workspace(rows: int, vocab: int, device="cuda") -> torch.Tensor:
+    """Workspace of sample_draw calls of at most these sizes; calls that may run at the
+    same time (on other streams, in other captured graphs) need one each."""
+    n = K.ks_sample_draw_workspace_bytes(rows, vocab)  # 0: the call reports the bad argument
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def sample_draw(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=None, top_p=None,
+                min_p=None, tokens=None, logprob=None, kept=None, workspace=None) -> torch.Tensor:
+    """One token per row of logits [rows, vocab] (float32 or bfloat16) from the given
+    uniforms u [rows], with every row's own settings (tensors [rows], None: 1 or off):
+    see ks_sample_draw.  Fills tokens (returned), logprob and kept where given."""
+    R, V = logits.shape
+    dev = logits.device
+    _need(logits.dtype in _DT and logits.stride(1) == 1 and dev.type == "cuda",
+          "logits must be float32 or bfloat16 [rows, vocab] on a GPU, dense rows")
+    if tokens is None:
+        tokens = torch.empty(R, dtype=torch.int32, device=dev)
+    for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32),
+                  (top_p, torch.float32), (min_p, torch.float32), (tokens, torch.int32),
+                  (logprob, torch.float32), (kept, torch.int32)):
+        _need(t is None or t.shape == (R,) and t.dtype == dt and t.is_contiguous()
+              and t.device == dev, f"settings and results must be dense [{R}] on the logits' "
+              "device: int32 top_k, tokens and kept, float32 the others")
+    if workspace is None:
+        workspace = sample_draw_workspace(R, V, dev)
+    p = lambda t: None if t is None else _ptr(t)  # noqa: E731
+    s = K.DrawParams(p(temperature), p(top_k), p(top_p), p(min_p), _ptr(u))
+    _here(dev, K.ks_sample_draw, _ptr(logits), _DT[logits.dtype], R, V,
+          logits.stride(0) if R > 1 else V, C.byref(s), _ptr(tokens), p(logprob), p(kept),
+          _ptr(workspace), workspace.numel())
+    return tokens
 
 
 class PagedCache:
