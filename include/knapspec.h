@@ -216,6 +216,8 @@ ks_status ks_pack_gate_up(const void* gate, const void* up, void* dst, int ffn, 
  * out [L][2 (K, V)][hkv][n_max][hd] in the model dtype; workspace is a device
  * buffer of ks_workspace_bytes(desc, lim) bytes.  Both stay caller-owned.
  * Fills the rotary table (float64 angles rounded to float32) on the stream.
+ * kv_cache may be NULL with kv_bytes 0: the context then has no cache until
+ * ks_use_paged gives it one, and the calls that need one fail with KS_ESTATE.
  */
 ks_status ks_create(const ks_model_desc* desc, const ks_limits* lim, const ks_weights* w,
                     void* kv_cache, size_t kv_bytes, void* workspace, size_t ws_bytes,
@@ -563,6 +565,22 @@ ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* r
                              const void* q, size_t ldq, void* out, size_t ldo, int hq, int dtype,
                              float scale, float* lse, void* workspace, size_t workspace_bytes,
                              void* stream);
+
+/*
+ * ks_use_paged: the context keeps its keys and values in pages from now on, for
+ * every call that uses a cache: layers (host array of L) are the layers' pages,
+ * table (device int32[table_len]) the page of each page / .. of positions, the same
+ * for all layers, for n_max positions at least.  layers = NULL: back to the buffer
+ * given to ks_create.  The table is read and checked once, here (synchronises the
+ * stream); it must stay as it is while it is in use.  Clears the decode state (then
+ * ks_prefill or ks_set_context).  hkv and hd must be the model's; kinds may differ
+ * by layer.  With KS_E4M3, a scale that a rejected draft token raised stays raised
+ * for its block, so a speculative run and an autoregressive one hold the same tokens
+ * to the same relative precision but not always to the same bits.
+ * ks_sublayer_apply with mode 0 then takes consecutive positions only.
+ */
+ks_status ks_use_paged(ks_ctx* ctx, const ks_paged_cache* layers, const int32_t* table,
+                       int table_len);
 
 /* Kernel classes of the decode step, for ks_profile_decode. */
 enum {

@@ -171,6 +171,7 @@ _SIG = {
                                                         _I]),
     "ks_paged_attention": (_I, [C.POINTER(PagedCache), C.POINTER(PagedRows), _P, C.c_size_t, _P,
                                 C.c_size_t, _I, _I, C.c_float, _P, _P, C.c_size_t, _P]),
+    "ks_use_paged": (_I, [_P, C.POINTER(PagedCache), _P, _I]),
     "ks_profile_decode": (_I, [_P, _P, _I, _I, C.POINTER(KernelProfile)]),
     "ks_time_launches": (_I, [_P, _P]),
     "ks_sublayer_apply": (_I, [_P, _I, _P, _P, _P, _I, _I]),
@@ -235,6 +236,7 @@ ks_sample_draw_workspace_bytes = lib.ks_sample_draw_workspace_bytes
 ks_paged_append = _wrap("ks_paged_append")
 ks_paged_attention = _wrap("ks_paged_attention")
 ks_paged_attention_workspace_bytes = lib.ks_paged_attention_workspace_bytes
+ks_use_paged = _wrap("ks_use_paged")
 ks_profile_decode = _wrap("ks_profile_decode")
 ks_time_launches = _wrap("ks_time_launches")
 ks_sublayer_apply = _wrap("ks_sublayer_apply")

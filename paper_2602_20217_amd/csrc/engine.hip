@@ -211,6 +211,9 @@ struct ks_ctx {
   float tau_conf = 0.f;                    // draft policy (ks_set_draft_policy)
   int gamma_source = KS_GAMMA_FIXED;
   ks_sampling samp{};                      // temperature <= 0: greedy
+  std::vector<PagedCache> pages;           // per layer (ks_use_paged), else empty
+  const int32_t* table = nullptr;          // their pages, by position
+  int table_len = 0;
 
   template <typename T>
   T* at(size_t off) const { return (T*)(ws + off); }
@@ -234,6 +237,13 @@ struct ks_ctx {
     return at<float>(y.stage) + ((size_t)i * (lim.gamma_max + 1) + k) * md.d;
   }
   bool sampling() const { return samp.temperature > 0.f; }
+  bool paged() const { return !pages.empty(); }
+  bool has_cache() const { return kv || paged(); }
+  // R rows of the context's one sequence on the pages of layer l
+  PagedRows page_rows(int l, int R, const int32_t* pos, int max_len) const {
+    const int most = std::min((long long)table_len * pages[l].page, (long long)md.n_max);
+    return PagedRows{1, R, nullptr, pos, table, table_len, R, std::min(max_len, most), nullptr};
+  }
   // sampling tables: row t of the target (verify) set, row gamma_max + 1 + t of
   // the draft set
   int32_t* tab_ids(int row) const { return at<int32_t>(y.tab_ids) + (size_t)row * KS_SAMPLE_KMAX; }
@@ -340,6 +350,65 @@ void resid_gemm(ks_ctx* c, int R, int K, Act A, const void* W, float* xout, cons
   run_gemm(c, g, batched, part_rows);
 }
 
+// q/k norms, RoPE and the key/value stores of R projected rows.
+void post_rows(ks_ctx* c, int l, int R, const int32_t* pos, int max_len, int mode) {
+  const ks_model_desc& d = c->md;
+  const float* qkv = c->at<float>(c->y.qkv);
+  const float* rope = c->at<float>(c->y.rope);
+  const int perm = c->bf() ? 1 : 0;  // the packed projection's column order
+  if (c->paged() && mode == 0) {
+    PagedAppend a{};
+    a.cache = c->pages[l];
+    a.rows = c->page_rows(l, R, pos, d.n_max);
+    a.q = qkv;
+    a.k = qkv + (size_t)d.hq * d.hd;
+    a.v = qkv + (size_t)(d.hq + d.hkv) * d.hd;
+    a.q_out = c->at<float>(c->y.q);
+    a.ldq = a.ldk = a.ldv = c->y.nqkv;
+    a.ldqo = (size_t)d.hq * d.hd;
+    a.hq = d.hq;
+    a.dtype = KS_F32;
+    a.rope = rope;
+    a.rope_rows = d.n_max;
+    if (d.qk_norm) {
+      a.q_gain = c->q_norm[l];
+      a.k_gain = c->k_norm[l];
+      a.eps = d.eps;
+    }
+    a.perm = perm;
+    PROF(c, KS_KC_QKV_POST, paged_append(a, c->st));
+    return;
+  }
+  QkvPostArgs qp{R, d.hq, d.hkv, d.hd, d.n_max, d.dtype, d.qk_norm, d.eps, qkv, rope,
+                 c->q_norm[l], c->k_norm[l], pos, c->at<float>(c->y.q),
+                 c->paged() ? nullptr : c->kc(l), c->paged() ? nullptr : c->vc(l),
+                 c->at<float>(c->y.kvself), mode, perm};
+  PROF(c, KS_KC_QKV_POST, qkv_post(qp, c->st));
+}
+
+// Split attention of the pages of layer l, into the partials that attn_combine reads.
+void paged_split(ks_ctx* c, int l, const AttnArgs& aa, bool batched) {
+  if (aa.max_len <= 0) return;
+  const ks_model_desc& d = c->md;
+  PagedAttn a{};
+  a.cache = c->pages[l];
+  a.rows = c->page_rows(l, aa.M, nullptr, aa.max_len);
+  a.q = aa.q;
+  a.ldq = (size_t)d.hq * d.hd;
+  a.hq = d.hq;
+  a.dtype = KS_F32;
+  // bf16 models: queries in two planes and probabilities in one, as on the flat cache
+  a.planes = c->bf() ? 2 : 3;
+  a.scale = 1.0f / std::sqrt((float)d.hd);
+  a.len = aa.len;
+  a.part = aa.part;
+  a.span = aa.span;
+  a.nsplit = (aa.max_len + aa.span - 1) / aa.span;
+  a.nsplit_ld = aa.nsplit;
+  a.few = !batched;
+  paged_attention(a, c->st);
+}
+
 // Attention sublayer of layer l on R rows: x_out = x_in + Wo attn(...).
 // mode 0: keys/values stored at pos; mode 1: own key/value (selection DP).
 // part_rows: rows that set the parts of the batched products' K sums (0: R).
@@ -352,32 +421,24 @@ void attn_rows(ks_ctx* c, int l, const float* xin, float* xout, int R, const int
   float* qkv = c->at<float>(c->y.qkv);
   float* q = c->at<float>(c->y.q);
   float* kvs = c->at<float>(c->y.kvself);
-  const float* rope = c->at<float>(c->y.rope);
   if (sk) {
     // without q/k norms and for cache writes, RoPE and the key/value stores
     // are the product's epilogue
-    const bool fused = mode == 0 && !d.qk_norm;
+    const bool fused = mode == 0 && !d.qk_norm && !c->paged();
     GemmArgs g = normed(c, R, c->y.nqkv, c->wqkv[l], fused ? EPI_QKV : EPI_STORE, qkv,
                         c->y.nqkv, Act{});
     if (fused)
-      g.qe = QkvEpi{d.hq, d.hkv, d.hd, d.n_max, rope, pos, q, (bf16_t*)c->kc(l),
-                    (bf16_t*)c->vc(l)};
+      g.qe = QkvEpi{d.hq, d.hkv, d.hd, d.n_max, c->at<float>(c->y.rope), pos, q,
+                    (bf16_t*)c->kc(l), (bf16_t*)c->vc(l)};
     PROF(c, KS_KC_GEMM_QKV, gemm_bf16_skinny(g, c->st));
-    if (!fused) {
-      QkvPostArgs qp{R, d.hq, d.hkv, d.hd, d.n_max, d.dtype, d.qk_norm, d.eps, qkv, rope,
-                     c->q_norm[l], c->k_norm[l], pos, q, c->kc(l), c->vc(l), kvs, mode, 1};
-      PROF(c, KS_KC_QKV_POST, qkv_post(qp, c->st));
-    }
+    if (!fused) post_rows(c, l, R, pos, max_len, mode);
   } else {
     PROF(c, KS_KC_NORM,
          norm_act(xin, d.d, c->attn_norm[l], d.eps, R, d.d, d.dtype, a1, c->st));
     PROF(c, KS_KC_GEMM_QKV,
          gemm(c, R, c->y.nqkv, d.d, a1, c->wqkv[l], EPI_STORE, qkv, c->y.nqkv, nullptr, 0,
               Act{}, batched, part_rows));
-    QkvPostArgs qp{R, d.hq, d.hkv, d.hd, d.n_max, d.dtype, d.qk_norm, d.eps, qkv, rope,
-                   c->q_norm[l], c->k_norm[l], pos, q, c->kc(l), c->vc(l), kvs, mode,
-                   c->bf() ? 1 : 0};
-    PROF(c, KS_KC_QKV_POST, qkv_post(qp, c->st));
+    post_rows(c, l, R, pos, max_len, mode);
   }
   const int tiles = batched ? BAT_TILES : dec_tiles(d.n_max, d.hkv);
   const int span = batched ? 64 * BAT_TILES : dec_span(d);
@@ -386,9 +447,13 @@ void attn_rows(ks_ctx* c, int l, const float* xin, float* xout, int R, const int
   for (int r0 = 0; r0 < R; r0 += step) {
     const int rr = std::min(step, R - r0);
     AttnArgs aa{rr, d.hq, d.hkv, d.hd, d.n_max, d.dtype,
-                q + (size_t)r0 * d.hq * d.hd, c->kc(l), c->vc(l), len + r0, max_len, tiles, span,
+                q + (size_t)r0 * d.hq * d.hd, c->paged() ? nullptr : c->kc(l),
+                c->paged() ? nullptr : c->vc(l), len + r0, max_len, tiles, span,
                 attn_rows_per_block(d.hq / d.hkv, batched), c->at<float>(c->y.part), ns};
-    PROF(c, KS_KC_ATTN, attn_split(aa, c->st));
+    if (c->paged())
+      PROF(c, KS_KC_ATTN, paged_split(c, l, aa, batched));
+    else
+      PROF(c, KS_KC_ATTN, attn_split(aa, c->st));
     Act out2 = a2;  // from row r0 (a multiple of 16)
     const size_t off = a2.kt ? (size_t)r0 * a2.kt * 64 : (size_t)r0 * a2.ld * (c->bf() ? 2 : 4);
     out2.hi = (char*)a2.hi + off;
@@ -655,6 +720,36 @@ ks_status ks_pack_gate_up(const void* gate, const void* up, void* dst, int ffn, 
   return KS_OK;
 }
 
+static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
+
+static ks_status check_paged(const ks_paged_cache* c, const ks_paged_rows* r, ks::PagedCache& pc,
+                             ks::PagedRows& pr) {
+  REQ(c && r, "null pointer");
+  REQ(c->kind == KS_BF16 || c->kind == KS_E4M3, "a paged cache holds KS_BF16 or KS_E4M3");
+  REQ(c->hd == 64 || c->hd == 128, "hd of a paged cache must be 64 or 128");
+  REQ(c->hkv >= 1 && c->n_pages >= 1, "hkv and n_pages must be positive");
+  REQ(c->page >= 16 && c->page <= 1024 && (c->page & (c->page - 1)) == 0,
+      "page must be a power of two in [16, 1024]");
+  const bool e4 = c->kind == KS_E4M3;
+  REQ(!e4 || (c->block >= 16 && c->block <= c->page && (c->block & (c->block - 1)) == 0),
+      "block must be a power of two in [16, page]");
+  REQ(r->B >= 0 && r->rows >= 0, "B and rows must be >= 0");
+  REQ(r->rows <= 1 << 30 && r->B <= 1 << 20, "too many rows or sequences");
+  if (r->B == 0 || r->rows == 0) return KS_OK;
+  REQ(c->k && c->v && (!e4 || (c->k_scale && c->v_scale)), "null cache pointer");
+  REQ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0, "cache buffers must be 16-byte aligned");
+  REQ(r->row_start && r->pos0 && r->table, "null pointer");
+  REQ(r->table_ld >= 1, "table_ld must be positive");
+  REQ(r->max_rows >= 1 && r->max_len >= 1, "max_rows and max_len must be positive");
+  pc = ks::PagedCache{c->k, c->v, c->k_scale, c->v_scale, c->n_pages, c->page, log2_of(c->page),
+                      e4 ? c->block : 16, e4 ? log2_of(c->block) : 4, c->hkv, c->hd, c->kind};
+  const long long most = std::min((long long)r->table_ld * c->page, 1ll << 30);
+  pr = ks::PagedRows{r->B, r->rows, r->row_start, r->pos0, r->table, r->table_ld,
+                     std::min(r->max_rows, r->rows), (int)std::min<long long>(r->max_len, most),
+                     r->err};
+  return KS_OK;
+}
+
 ks_status ks_create(const ks_model_desc* desc, const ks_limits* lim, const ks_weights* w,
                     void* kv_cache, size_t kv_bytes, void* workspace, size_t ws_bytes,
                     void* stream, ks_ctx** out) {
@@ -662,7 +757,9 @@ ks_status ks_create(const ks_model_desc* desc, const ks_limits* lim, const ks_we
   if (s != KS_OK) return s;
   s = check_lim(lim);
   if (s != KS_OK) return s;
-  REQ(w && out && kv_cache && workspace, "null pointer");
+  // no cache at all: the context runs on pages (ks_use_paged)
+  const bool no_cache = !kv_cache && kv_bytes == 0;
+  REQ(w && out && (kv_cache || no_cache) && workspace, "null pointer");
   REQ(w->embed && w->lm_head && w->final_norm && w->attn_norm && w->wqkv && w->wo &&
           w->mlp_norm && w->w_gate_up && w->w_down,
       "null weight pointer");
@@ -673,7 +770,7 @@ ks_status ks_create(const ks_model_desc* desc, const ks_limits* lim, const ks_we
     if (desc->qk_norm) REQ(w->q_norm && w->k_norm && w->q_norm[l] && w->k_norm[l], "qk_norm gains missing");
   }
   const Layout y = make_layout(*desc, *lim);
-  if (kv_bytes < ks_kv_cache_bytes(desc)) {
+  if (!no_cache && kv_bytes < ks_kv_cache_bytes(desc)) {
     set_error("kv cache smaller than ks_kv_cache_bytes");
     return KS_ENOMEM;
   }
@@ -736,6 +833,10 @@ ks_status ks_prefill(ks_ctx* c, const int32_t* tokens, int n, int32_t* out_first
     return KS_ECAPACITY;
   }
   for (int t = 0; t < n; ++t) REQ(tokens[t] >= 0 && tokens[t] < d.vocab, "token id out of range");
+  if (!c->has_cache()) {
+    set_error("the context has no cache: ks_use_paged first");
+    return KS_ESTATE;
+  }
   const int FR = c->lim.prefill_chunk;
   const int r0 = std::min(n, c->lim.m_rounds * (c->lim.gamma_max + 1));
   float* x = c->at<float>(c->y.x);
@@ -783,6 +884,10 @@ ks_status ks_prefill(ks_ctx* c, const int32_t* tokens, int n, int32_t* out_first
 ks_status ks_set_context(ks_ctx* c, int n_cached, int32_t last_token) {
   REQ(c, "ctx is null");
   REQ(n_cached >= 0, "n_cached must be >= 0");
+  if (!c->has_cache()) {
+    set_error("the context has no cache: ks_use_paged first");
+    return KS_ESTATE;
+  }
   if (n_cached >= c->md.n_max) {
     set_error("n_cached exceeds the KV cache");
     return KS_ECAPACITY;
@@ -793,6 +898,45 @@ ks_status ks_set_context(ks_ctx* c, int n_cached, int32_t last_token) {
   c->k_draft = 0;
   c->blocks.clear();
   c->ready = true;
+  return KS_OK;
+}
+
+ks_status ks_use_paged(ks_ctx* c, const ks_paged_cache* layers, const int32_t* table,
+                       int table_len) {
+  REQ(c, "ctx is null");
+  std::vector<PagedCache> pages;
+  if (layers) {
+    REQ(table && table_len >= 1, "table is empty");
+    int least = INT32_MAX, fewest = INT32_MAX;  // page size, pages
+    for (int l = 0; l < c->md.L; ++l) {
+      // the rows stand for what the context will pass
+      const ks_paged_rows r{1, 1, table, table, table, table_len, 1, c->md.n_max, nullptr};
+      PagedCache pc{};
+      PagedRows pr{};
+      const ks_status s = check_paged(&layers[l], &r, pc, pr);
+      if (s != KS_OK) return s;
+      REQ(layers[l].hkv == c->md.hkv && layers[l].hd == c->md.hd,
+          "hkv and hd of the pages must be the model's");
+      pages.push_back(pc);
+      least = std::min(least, pc.page);
+      fewest = std::min(fewest, pc.n_pages);
+      if ((long long)table_len * pc.page < c->md.n_max) {
+        set_error("the table holds fewer positions than n_max");
+        return KS_ECAPACITY;
+      }
+    }
+    std::vector<int32_t> host(table_len);
+    HIPCHK(hipMemcpyAsync(host.data(), table, (size_t)table_len * 4, hipMemcpyDeviceToHost, c->st));
+    HIPCHK(hipStreamSynchronize(c->st));
+    for (int i = 0; i < (c->md.n_max + least - 1) / least; ++i)
+      REQ(host[i] >= 0 && host[i] < fewest, "a page of the table is out of range");
+  }
+  c->pages = pages;
+  c->table = layers ? table : nullptr;
+  c->table_len = layers ? table_len : 0;
+  c->ready = false;
+  c->k_draft = 0;
+  c->blocks.clear();
   return KS_OK;
 }
 
@@ -1042,36 +1186,6 @@ ks_status ks_sample_draw(const void* logits, int dtype, int rows, int vocab, siz
                              p->min_p, p->u, tokens, logprob, kept, workspace},
                 (hipStream_t)stream);
   HIPCHK(hipGetLastError());
-  return KS_OK;
-}
-
-static int log2_of(int x) { return 31 - __builtin_clz((unsigned)x); }
-
-static ks_status check_paged(const ks_paged_cache* c, const ks_paged_rows* r, ks::PagedCache& pc,
-                             ks::PagedRows& pr) {
-  REQ(c && r, "null pointer");
-  REQ(c->kind == KS_BF16 || c->kind == KS_E4M3, "a paged cache holds KS_BF16 or KS_E4M3");
-  REQ(c->hd == 64 || c->hd == 128, "hd of a paged cache must be 64 or 128");
-  REQ(c->hkv >= 1 && c->n_pages >= 1, "hkv and n_pages must be positive");
-  REQ(c->page >= 16 && c->page <= 1024 && (c->page & (c->page - 1)) == 0,
-      "page must be a power of two in [16, 1024]");
-  const bool e4 = c->kind == KS_E4M3;
-  REQ(!e4 || (c->block >= 16 && c->block <= c->page && (c->block & (c->block - 1)) == 0),
-      "block must be a power of two in [16, page]");
-  REQ(r->B >= 0 && r->rows >= 0, "B and rows must be >= 0");
-  REQ(r->rows <= 1 << 30 && r->B <= 1 << 20, "too many rows or sequences");
-  if (r->B == 0 || r->rows == 0) return KS_OK;
-  REQ(c->k && c->v && (!e4 || (c->k_scale && c->v_scale)), "null cache pointer");
-  REQ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) == 0, "cache buffers must be 16-byte aligned");
-  REQ(r->row_start && r->pos0 && r->table, "null pointer");
-  REQ(r->table_ld >= 1, "table_ld must be positive");
-  REQ(r->max_rows >= 1 && r->max_len >= 1, "max_rows and max_len must be positive");
-  pc = ks::PagedCache{c->k, c->v, c->k_scale, c->v_scale, c->n_pages, c->page, log2_of(c->page),
-                      e4 ? c->block : 16, e4 ? log2_of(c->block) : 4, c->hkv, c->hd, c->kind};
-  const long long most = std::min((long long)r->table_ld * c->page, 1ll << 30);
-  pr = ks::PagedRows{r->B, r->rows, r->row_start, r->pos0, r->table, r->table_ld,
-                     std::min(r->max_rows, r->rows), (int)std::min<long long>(r->max_len, most),
-                     r->err};
   return KS_OK;
 }
 
@@ -1398,6 +1512,10 @@ ks_status ks_sublayer_apply(ks_ctx* c, int i, const float* x_in, float* x_out, c
   REQ(i >= 1 && i <= 2 * d.L, "sublayer index out of range");
   REQ(R >= 1 && R <= c->y.XR, "R out of range");
   REQ(mode == 0 || mode == 1, "mode must be 0 or 1");
+  if (!c->has_cache()) {
+    set_error("the context has no cache: ks_use_paged first");
+    return KS_ESTATE;
+  }
   int mx = 0;
   std::vector<int32_t> hl(R);
   for (int t = 0; t < R; ++t) {
@@ -1406,6 +1524,8 @@ ks_status ks_sublayer_apply(ks_ctx* c, int i, const float* x_in, float* x_out, c
       set_error("position exceeds the KV cache");
       return KS_ECAPACITY;
     }
+    REQ(!c->paged() || mode == 1 || pos[t] == pos[0] + t,
+        "rows stored to pages lie at consecutive positions");
     hl[t] = pos[t] + (mode == 0 ? 1 : 0);
     mx = std::max(mx, hl[t]);
   }

@@ -267,6 +267,9 @@ struct PagedAttn {
   const int32_t* len;  // device [rows] or nullptr
   float* part;         // [rows][hq][nsplit_ld][hd + 2], nullptr: one split
   int nsplit, nsplit_ld, span;
+  // bf16 planes of queries: 1 (bf16), 3 (float32), or 2 with probabilities in one
+  int planes = 0;    // 0: by dtype
+  bool few = false;  // split kernel whatever the number of rows
   int col_max = 0, cblocks = 0;  // set by paged_attention
 };
 void paged_attention(const PagedAttn& a, hipStream_t st);

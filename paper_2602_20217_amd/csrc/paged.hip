@@ -194,7 +194,9 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
   const size_t head = (size_t)pid * c.hkv + h;
   const bool is_k = wave < 2;
   const int row_of = sr.r0 - p0;  // row of position p: row_of + p
+  const int d = threadIdx.x - 128;  // value waves: the thread's dimension
   const T* src = (const T*)(is_k ? a.k : a.v) + (size_t)h * HD;
+  if (!is_k) src += a.perm && d < HD ? qkv_perm(d, HD) : min(d, HD - 1);
   const size_t ld = is_k ? a.ldk : a.ldv;
 
   float s = 1.f, inv = 1.f, ratio = 1.f;
@@ -212,9 +214,9 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
         if (finite_f(y.x)) amax = fmaxf(amax, fabsf(y.x));
         if (finite_f(y.y)) amax = fmaxf(amax, fabsf(y.y));
       }
-    } else if ((int)threadIdx.x - 128 < HD) {
+    } else if (d < HD) {
       for (int p = n0; p < n1; ++p) {
-        const float y = ld1(src + (size_t)(row_of + p) * ld + (threadIdx.x - 128));
+        const float y = ld1(src + (size_t)(row_of + p) * ld);
         if (finite_f(y)) amax = fmaxf(amax, fabsf(y));
       }
     }
@@ -261,7 +263,6 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
     }
     return;
   }
-  const int d = threadIdx.x - 128;
   if (d >= HD) return;
   for (int g0 = bs; g0 < n1; g0 += GRAN) {  // granules that the block's tokens reach
     if (g0 + GRAN <= n0 && (!E4 || ratio == 1.f)) continue;
@@ -277,7 +278,7 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
         if (p < n0) {
           if (ratio != 1.f) cd = code_of(value_of(cd) * ratio);
         } else if (p < n1) {
-          cd = code_of(ld1(src + (size_t)(row_of + p) * ld + d) * inv);
+          cd = code_of(ld1(src + (size_t)(row_of + p) * ld) * inv);
         }
         w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
       }
@@ -286,7 +287,7 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
       bf16_t* vc = (bf16_t*)c.v + off;
       for (int i = 0; i < GRAN; ++i) {
         const int p = g0 + i;
-        if (p >= n0 && p < n1) vc[i] = f2bf(ld1(src + (size_t)(row_of + p) * ld + d));
+        if (p >= n0 && p < n1) vc[i] = f2bf(ld1(src + (size_t)(row_of + p) * ld));
       }
     }
   }
@@ -328,7 +329,7 @@ __device__ inline int dim_of(int s, int g) {
 }
 
 // 8 query elements as QP bf16 planes that add up to them: one plane holds bf16
-// queries exactly, three hold float32 ones to 24 bits
+// queries exactly, two hold float32 ones to 16 bits and three to 24
 template <int QP>
 __device__ inline void load_q(const void* p, bool f32, bf16x8 (&o)[QP]) {
   if (QP == 1) {
@@ -369,7 +370,7 @@ __device__ inline uint32_t bytes_below(int n) {  // mask of the first n of 4 byt
 // shortest and the longest length hold one, the rows are added one at a time.
 template <int HD, bool E4, int QP, int CB>
 __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
-  constexpr int PP = QP;               // probability planes, as of the queries
+  constexpr int PP = QP == 3 ? 3 : 1;  // probability planes
   constexpr int NS = HD / 32;          // contraction steps of a score
   constexpr int ND = HD / 16;          // blocks of 16 output dims
   constexpr int RS = HD + 4;           // LDS merge record per column (bank-shifted)
@@ -543,8 +544,8 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
         for (int v = 0; v < 4; ++v) {
           const float e = __builtin_amdgcn_exp2f(s[cb][kt][v] - mn);
           sum += e;
-          // one plane (bf16 rows) holds a probability to 2^-8, as the output is held;
-          // three (float32 rows) to 2^-24 (two, 2^-16, lose digits of the output)
+          // one plane holds a probability to 2^-8, as a bf16 output is held; three
+          // (float32 rows) to 2^-24 (two, 2^-16, lose digits of the output)
           float r = e;
 #pragma unroll
           for (int n = 0; n < PP; ++n) {
@@ -806,7 +807,9 @@ void paged_attention(const PagedAttn& a_, hipStream_t st) {
     else if (c.kind == KS_E4M3) KS_DEC(64, true, QP_);                 \
     else KS_DEC(64, false, QP_);                                       \
   } while (0)
-  if (a.dtype == KS_BF16) KS_DEC_T(1);
+  const int planes = a.planes ? a.planes : a.dtype == KS_BF16 ? 1 : 3;
+  if (planes == 1) KS_DEC_T(1);
+  else if (planes == 2) KS_DEC_T(2);
   else KS_DEC_T(3);
 #undef KS_DEC_T
 #undef KS_DEC

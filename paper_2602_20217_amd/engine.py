@@ -47,10 +47,15 @@ class DeviceModel:
     dtype ("f32" or "bf16").  Call ``upload(kind, layer, array)`` for every weight
     (kinds embed, lm_head, wq, wk, wv, wo, w_gate, w_up, w_down; row-major [out, in]
     float32 arrays, bf16-valued for bf16 models), then ``finalize()``.
+
+    cache: "flat" (the model's type, contiguous), or pages of 64 tokens of "bf16" or
+    of "e4m3" (8 bits, a scale for every 16 tokens and head: half the bytes of bf16);
+    ``use_paged`` gives the context other pages.
     """
 
     def __init__(self, cfg, n_max: int, gamma_max: int = 8, m_rounds: int = 5,
-                 cap_max: int = 256, prefill_chunk: int = 256, device: str = "cuda:0"):
+                 cap_max: int = 256, prefill_chunk: int = 256, device: str = "cuda:0",
+                 cache: str = "flat"):
         self.cfg = cfg
         self.dev = torch.device(device)
         self.bf = cfg.dtype == "bf16"
@@ -63,7 +68,8 @@ class DeviceModel:
         wsb = K.ks_workspace_bytes(C.byref(self.desc), C.byref(self.lim))
         if kvb == 0 or wsb == 0:
             raise K.KsError(K.KS_EINVAL, K.last_error())
-        self.kv = torch.zeros(kvb, dtype=torch.uint8, device=self.dev)
+        self._cache_kind = cache
+        self.kv = torch.zeros(kvb if cache == "flat" else 0, dtype=torch.uint8, device=self.dev)
         self.ws = torch.zeros(wsb, dtype=torch.uint8, device=self.dev)
         wdt = torch.int16 if self.bf else torch.float32
         L, d = cfg.L, cfg.d
@@ -150,9 +156,14 @@ class DeviceModel:
                                  cast(A["w_down"]))
         ctx = C.c_void_p()
         K.ks_create(C.byref(self.desc), C.byref(self.lim), C.byref(self.weights),
-                    _ptr(self.kv), self.kv.numel(), _ptr(self.ws), self.ws.numel(), _stream(),
-                    C.byref(ctx))
+                    _ptr(self.kv) or None, self.kv.numel(), _ptr(self.ws), self.ws.numel(),
+                    _stream(), C.byref(ctx))
         self.ctx = ctx
+        if self._cache_kind != "flat":
+            n = (self.desc.n_max + 63) // 64
+            self.use_paged([PagedCache(n, 64, self.cfg.hkv, self.cfg.hd, self._cache_kind,
+                                       device=self.dev) for _ in range(self.cfg.L)],
+                           torch.arange(n, dtype=torch.int32, device=self.dev))
         torch.cuda.current_stream().synchronize()
         return self
 
@@ -172,7 +183,9 @@ class DeviceModel:
         wsb = K.ks_workspace_bytes(C.byref(other.desc), C.byref(other.lim))
         if kvb == 0 or wsb == 0:
             raise K.KsError(K.KS_EINVAL, K.last_error())
-        other.kv = torch.zeros(kvb, dtype=torch.uint8, device=self.dev)
+        other._cache_kind = self._cache_kind
+        other.kv = torch.zeros(kvb if self._cache_kind == "flat" else 0, dtype=torch.uint8,
+                               device=self.dev)
         other.ws = torch.zeros(wsb, dtype=torch.uint8, device=self.dev)
         other.w, other.gains = self.w, self.gains
         other._pending, other._done = {}, set(self._done)
@@ -201,6 +214,23 @@ class DeviceModel:
         kk = self.kv[base:base + n].view(dt).view(c.hkv, self.desc.n_max, c.hd)
         vv = self.kv[base + n:base + 2 * n].view(dt).view(c.hkv, self.desc.n_max, c.hd)
         return kk, vv
+
+    def use_paged(self, layers, table: torch.Tensor):
+        """Keys and values in pages from now on (see ks_use_paged): layers, one
+        PagedCache each, and the int32 table of the sequence's pages, n_max positions
+        at least.  layers = None: back to the flat cache."""
+        if layers is None:
+            K.ks_use_paged(self.ctx, None, None, 0)
+            self.pages = self.page_table = None
+            return
+        if len(layers) != self.cfg.L or any(c.device != self.dev for c in layers):
+            raise ValueError("one PagedCache per layer, on the model's device")
+        if (table.dim() != 1 or table.dtype != torch.int32 or not table.is_contiguous()
+                or table.device != self.dev):
+            raise ValueError("table must be a dense int32 vector on the model's device")
+        arr = (K.PagedCache * len(layers))(*[c.desc for c in layers])
+        K.ks_use_paged(self.ctx, arr, _ptr(table), table.numel())
+        self.pages, self.page_table = list(layers), table  # kept alive
 
     # ------------------------------------------------------------ decode calls
     def prefill(self, tokens) -> int:
