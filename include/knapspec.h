@@ -536,8 +536,9 @@ typedef struct ks_paged_rows {
  * ldqo = ldq).  q_out is 0 for padding and for rows past rope_rows.
  * KS_E4M3: a block's scale is the smallest power of two s (at least 2^-100) with
  * every finite new |element| <= 448 s, or the scale it has, if it holds earlier
- * tokens of the sequence (those below pos0[b]) and that is larger; if it grows, their
- * codes are rounded to the new scale.  Codes are rounded to nearest, ties to even;
+ * tokens of the sequence (those below pos0[b]) and that is larger (a scale that is
+ * not a positive finite number counts as none); if it grows, their codes are rounded
+ * to the new scale.  Codes are rounded to nearest, ties to even;
  * an element that is not finite becomes NaN.  Tokens of a block at or past the new
  * ones have undefined codes.  Appending the same rows again stores the same.
  * Asynchronous on stream.
@@ -552,7 +553,8 @@ ks_status ks_paged_append(const ks_paged_cache* cache, const ks_paged_rows* rows
  * 128.  q and out [rows][hq][hd] of dtype, rows ldq and ldo elements apart, 16-byte
  * aligned (ldq and ldo too).  KS_F32: to float32 precision; KS_BF16: probabilities
  * are rounded to bf16 before they meet the values.  A row that attends nothing (at
- * a negative position, or all of its pages invalid) gets zeros, and lse -inf.  Values
+ * a negative position, all of its pages invalid, every score -inf) gets zeros, and
+ * lse -inf.  Values
  * and keys past a row's position do not reach it, whatever they hold.  lse: float32
  * [rows][hq] or NULL, log of the sum of exp(scale q.k).  scale must be finite.
  * workspace: ks_paged_attention_workspace_bytes() bytes; nothing in it needs to

@@ -203,7 +203,8 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
   if (E4) {
     __shared__ float s_max[4];
     float* sp = (is_k ? c.k_scale : c.v_scale) + (head << (c.lpage - lblock)) + (s0 >> lblock);
-    const float s_old = n0 > bs ? *sp : 0.f;  // earlier tokens only
+    float s_old = n0 > bs ? *sp : 0.f;  // earlier tokens only
+    if (!(s_old > 0.f && s_old <= FLT_MAX)) s_old = 0.f;
     float amax = 0.f;
     if (is_k) {
       for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
@@ -328,8 +329,27 @@ __device__ inline int dim_of(int s, int g) {
   return E4 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
 }
 
-// 8 query elements as QP bf16 planes that add up to them: one plane holds bf16
-// queries exactly, two hold float32 ones to 16 bits and three to 24
+// x as N bf16 planes that add up to it, 8 bits each.  All have x's sign and none is 0
+// unless x is: times an infinite key or value every plane then gives the infinity
+// that x gives, where opposite ones or a 0 among them would give NaN.  (2^-126 in
+// the place of 0 is below what float32 keeps of any sum here.)
+template <int N>
+__device__ inline void planes_of(float x, __bf16 (&o)[N]) {
+  float r = x;
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    if (n + 1 < N)
+      o[n] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(r) >> 16));  // towards 0
+    else
+      o[n] = (__bf16)r;
+    r -= (float)o[n];
+    if (n > 0 && x != 0.f && (float)o[n] == 0.f)
+      o[n] = (__bf16)copysignf(1.17549435e-38f, x);
+  }
+}
+
+// 8 query elements as QP bf16 planes: one holds bf16 queries exactly, two hold
+// float32 ones to 16 bits and three to 24
 template <int QP>
 __device__ inline void load_q(const void* p, bool f32, bf16x8 (&o)[QP]) {
   if (QP == 1) {
@@ -340,12 +360,10 @@ __device__ inline void load_q(const void* p, bool f32, bf16x8 (&o)[QP]) {
   const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    float r = x[e];
+    __bf16 y[QP];
+    planes_of<QP>(x[e], y);
 #pragma unroll
-    for (int n = 0; n < QP; ++n) {
-      o[n][e] = (__bf16)r;
-      r -= (float)o[n][e];
-    }
+    for (int n = 0; n < QP; ++n) o[n][e] = y[n];
   }
 }
 
@@ -546,12 +564,10 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
           sum += e;
           // one plane holds a probability to 2^-8, as a bf16 output is held; three
           // (float32 rows) to 2^-24 (two, 2^-16, lose digits of the output)
-          float r = e;
+          __bf16 y[PP];
+          planes_of<PP>(e, y);
 #pragma unroll
-          for (int n = 0; n < PP; ++n) {
-            p[cb][kt >> 1][n][4 * (kt & 1) + v] = (__bf16)r;
-            r -= (float)p[cb][kt >> 1][n][4 * (kt & 1) + v];
-          }
+          for (int n = 0; n < PP; ++n) p[cb][kt >> 1][n][4 * (kt & 1) + v] = y[n];
         }
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
@@ -686,15 +702,16 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
       if (d == 0) *(float2*)(x + HD) = make_float2(mm * LN2, ll);
       continue;
     }
-    const float inv = n > 0 ? 1.0f / ll : 0.f;
+    const bool any = ll != 0.f;  // else the row attends nothing
+    const float inv = 1.0f / ll;
     const size_t at = r * a.ldo + (size_t)h * HD + d;
 #pragma unroll
     for (int v = 0; v < 4; ++v) {
-      const float y = n > 0 ? oo[v] * inv : 0.f;
+      const float y = any ? oo[v] * inv : 0.f;
       if (QP == 1) ((bf16_t*)a.out)[at + v] = f2bf(y);
       else ((float*)a.out)[at + v] = y;
     }
-    if (d == 0 && a.lse) a.lse[r * a.hq + h] = n > 0 ? mm * LN2 + logf(ll) : -INFINITY;
+    if (d == 0 && a.lse) a.lse[r * a.hq + h] = any ? mm * LN2 + logf(ll) : -INFINITY;
   }
 }
 
@@ -746,10 +763,11 @@ __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
     }
   }
   T* dst = (T*)a.out + (size_t)r * a.ldo + (size_t)h * HD + DPL * lane;
+  const bool any = l != 0.f;
   const float inv = 1.0f / l;
 #pragma unroll
-  for (int e = 0; e < DPL; ++e) st1(dst + e, n > 0 ? o[e] * inv : 0.f);
-  if (lane == 0 && a.lse) a.lse[(size_t)r * a.hq + h] = n > 0 ? m + logf(l) : -INFINITY;
+  for (int e = 0; e < DPL; ++e) st1(dst + e, any ? o[e] * inv : 0.f);
+  if (lane == 0 && a.lse) a.lse[(size_t)r * a.hq + h] = any ? m + logf(l) : -INFINITY;
 }
 
 }  // namespace

@@ -278,3 +278,269 @@ def test_steps(E, c):
     x.step([1] * B, std=9.0, tail=3)  # larger: its scale grows
     x.step([(b * 3) % 5 for b in range(B)], std=2.0)
     x.step([min(11, cap - int(n)) for n in x.len], rope=False)
+
+
+SMALL = (3, 8, 2, 128, 32, 16, "e4m3", "bf16", 4)
+
+
+def forget(x, n):
+    """The tokens of the sequences from n[b] on are no longer theirs."""
+    for b in range(x.B):
+        for p in range(int(n[b]), x.table.shape[1] * x.cache.page):
+            x.plain.known[x.table[b, p // x.cache.page], p % x.cache.page] = False
+        x.len[b] = min(x.len[b], n[b])
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "bf16"])
+def test_rollback_and_padding(E, kind):
+    """Rejected rows are overwritten; rows at negative positions are padding."""
+    x = Case(E, *SMALL[:6], kind, *SMALL[7:], seed=5)
+    qo, out, lse = x.step([5, 40, 7], pos0=[-2, 0, -7])
+    assert bool((qo[:2] == 0).all()) and bool((out[:2] == 0).all())
+    assert bool((out[45:] == 0).all()) and bool(torch.isneginf(lse[45:]).all())
+    for n, std in (([5, 5, 5], 1.0), ([5, 5, 5], 4.0), ([3, 1, 2], 1.0), ([1, 1, 1], 0.5)):
+        x.step(n, std)
+        keep = np.maximum(x.len - [2, 4, 0], 0)
+        forget(x, keep)
+    x.step([2, 3, 4])
+
+
+def test_same_rows_again_and_no_queries(E):
+    x = Case(E, *SMALL, seed=6)
+    x.step([9, 21, 40])
+    (q, k, v), _ = x.rows(6)
+    args = (x.cache, i32(x.table), i32([0, 1, 4, 6]), i32(x.len), k, v)
+    assert E.paged_append(*args) is None
+    was = [t.view(torch.uint8).clone() for t in (x.cache.k, x.cache.v)] + \
+        [x.cache.k_scale.clone(), x.cache.v_scale.clone()]
+    qc = q.contiguous()
+    ref = E.paged_append(*args, q=qc, rope=None)
+    assert torch.equal(ref, qc)
+    now = [t.view(torch.uint8) for t in (x.cache.k, x.cache.v)] + [x.cache.k_scale, x.cache.v_scale]
+    assert all(torch.equal(a.nan_to_num(-1) if a.is_floating_point() else a,
+                           b.nan_to_num(-1) if b.is_floating_point() else b)
+               for a, b in zip(was, now))
+    rope = torch.from_numpy(x.rope).cuda()
+    ref = E.paged_append(*args, q=qc, rope=rope)
+    got = E.paged_append(*args, q=qc, rope=rope, q_out=qc)  # in place
+    assert got is qc and torch.equal(ref, qc)
+
+
+@pytest.mark.parametrize("std", [1e-40, 1e-33, 1e30])
+def test_magnitudes(E, std):
+    """Scales down to 2^-100 and values near the float32 limits."""
+    x = Case(E, 2, 2, 1, 64, 16, 16, "e4m3", "f32", 3, seed=7)
+    start, pos0 = [0, 20, 25], [0, 3]
+    (q, k, v), (_, fk, fv) = x.rows(25, std)
+    E.paged_append(x.cache, i32(x.table), i32(start), i32(pos0), k, v)
+    x.plain.append(x.table, start, pos0, fk, fv, None)
+    gk, gv = values(x.cache)
+    for got, ref in ((gk, x.plain.k), (gv, x.plain.v)):
+        for pg, sl in zip(*np.nonzero(x.plain.known)):
+            assert np.array_equal(got[pg, :, sl], ref[pg, :, sl])
+
+
+def test_bad_pages_are_left_out(E):
+    x = Case(E, *SMALL, seed=8)
+    x.step([60, 33, 50])
+    was = [t.view(torch.uint8).clone() for t in (x.cache.k, x.cache.v)]
+    tab = x.table.copy()
+    tab[0, 1] = -1          # holds positions 32..59 of sequence 0
+    tab[2, 0] = 14          # n_pages is 14
+    tab[2, 1] = 2 ** 31 - 1
+    start, pos0 = [0, 2, 4, 5], [60, 33, 50]
+    (q, k, v), (fq, fk, fv) = x.rows(5)
+    err = torch.zeros(3, dtype=torch.int32, device="cuda")
+    E.paged_append(x.cache, i32(tab), i32(start), i32(pos0), k, v, err=err)
+    assert err.tolist() == [1, 0, 1]
+    err.zero_()
+    qo, lse = q.contiguous(), torch.zeros(5, 8, device="cuda")
+    out = E.paged_attention(x.cache, i32(tab), i32(start), i32(pos0), qo, lse=lse, err=err)
+    assert err.tolist() == [1, 0, 1]
+    for a, t in zip(was, (x.cache.k, x.cache.v)):  # only sequence 1's page was written
+        t = t.view(torch.uint8)
+        other = [p for p in range(14) if p != tab[1, 1]]
+        assert torch.equal(a[other], t[other])
+    p = Plain.__new__(Plain)
+    p.__dict__.update(x.plain.__dict__)
+    p.k, p.v = values(x.cache)
+    t2 = tab.copy()
+    t2[2, 1] = -1
+    x.plain.append(x.table, [0, 0, 2, 2], pos0, fk[2:4], fv[2:4], None)
+    ro, rl = p.attend(t2, start, pos0, fq, 128 ** -0.5)
+    assert np.abs(out.double().cpu().numpy() - ro).max() <= 2.0 ** -6 * 4
+    assert bool((out[4] == 0).all()) and bool(torch.isneginf(lse[4]).all())
+
+
+def test_bounds_that_do_not_hold(E):
+    """More rows than max_rows, positions past max_len, past the table, past the
+    rotation table: left out and reported, nothing else touched."""
+    x = Case(E, *SMALL, seed=9)
+    x.step([60, 33, 50])
+    (q, k, v), (fq, _, _) = x.rows(12)
+    tab, start, pos0 = i32(x.table), [0, 2, 8, 12], [60, 33, 50]
+    q = q.contiguous()
+
+    def attend(**kw):
+        err = torch.zeros(3, dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 7.0)
+        E.paged_attention(x.cache, tab, i32(start), i32(kw.pop("pos0", pos0)), q, out=out, err=err, **kw)
+        return out, err.tolist()
+
+    full, err = attend(pos0=[58, 20, 40])
+    assert err == [0, 0, 0]
+    out, err = attend(pos0=[58, 20, 40], max_rows=4)
+    assert err == [0, 1, 0] and bool((out[6:8] == 7).all())
+    ok = [0, 1, 2, 3, 4, 5, 8, 9, 10, 11]
+    assert (out[ok] - full[ok]).abs().max() <= 2.0 ** -6
+    out, err = attend(pos0=[58, 20, 40], max_len=43)
+    assert err == [1, 0, 1]
+    assert (out[2:8] - full[2:8]).abs().max() <= 2.0 ** -6
+    assert (out[8:11] - full[8:11]).abs().max() <= 2.0 ** -6  # positions 40..42
+    out, err = attend(pos0=[2 ** 31 - 1, 20, -2 ** 31])
+    assert err == [1, 0, 0] and bool((out[8:] == 0).all())
+    err = torch.zeros(3, dtype=torch.int32, device="cuda")
+    was = [t.view(torch.uint8).clone() for t in (x.cache.k, x.cache.v)]
+    rope = torch.from_numpy(x.rope).cuda()
+    qo = E.paged_append(x.cache, tab, i32(start), i32([2 ** 31 - 1, -2 ** 31, 128]), k, v, q=q,
+                        rope=rope, err=err)
+    assert err.tolist() == [1, 0, 1] and bool((qo == 0).all())
+    assert all(torch.equal(a, t.view(torch.uint8)) for a, t in zip(was, (x.cache.k, x.cache.v)))
+    # garbage row boundaries stay inside the tensors
+    E.paged_attention(x.cache, tab, i32([-5, 400, 3, 2 ** 31 - 1]), i32(pos0), q)
+    E.paged_append(x.cache, tab, i32([2 ** 31 - 1, -2 ** 31, 1000, 5]), i32(pos0), k, v, q=q)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("kind,dtype,hd", [("e4m3", "bf16", 128), ("bf16", "bf16", 128),
+                                           ("bf16", "f32", 64), ("e4m3", "f32", 64)])
+@pytest.mark.parametrize("many", [False, True])
+def test_infinities_and_nan(E, kind, dtype, hd, many):
+    """What is not finite reaches the rows that attend it and no others."""
+    x = Case(E, 2, 4, 2, hd, 32, 16, kind, dtype, 8, seed=10)
+    x.step([70, 20])
+    n = [90, 6] if many else [5, 6]
+    start, pos0 = np.cumsum([0] + n), x.len.copy()
+    (q, k, v), (fq, fk, fv) = x.rows(sum(n))
+    a, b = (k.clone(), v.clone())
+    a[3, 1, 5] = math.inf
+    b[2, 0, 7] = math.nan
+    b[4, 1, 9] = math.inf
+    b[n[0] + 1, 0, 0] = -math.inf
+    b[n[0] + 3, 0, 0] = math.inf
+    a[n[0] + 5, 1, 0] = math.nan
+    E.paged_append(x.cache, i32(x.table), i32(start), i32(pos0), a, b)
+    for i in range(2):
+        for p in range(pos0[i], pos0[i] + n[i]):
+            x.plain.known[x.table[i, p // 32], p % 32] = True
+    lse = torch.zeros(sum(n), 4, device="cuda")
+    out = E.paged_attention(x.cache, i32(x.table), i32(start), i32(pos0), q, lse=lse,
+                            **(dict() if many else dict(max_rows=6)))
+    assert bool(torch.isfinite(out[:2]).all()) and not bool(torch.isfinite(out[2]).all())
+    p = Plain.__new__(Plain)
+    p.__dict__.update(x.plain.__dict__)
+    p.k, p.v = values(x.cache)
+    with np.errstate(invalid="ignore"):
+        ro, rl = p.attend(x.table, start, pos0, fq, hd ** -0.5)
+    o = out.double().cpu().numpy()
+    assert np.array_equal(np.isnan(o), np.isnan(ro))
+    inf = np.isinf(ro)
+    assert np.array_equal(o[inf], ro[inf])
+    fin = np.isfinite(ro)
+    assert np.abs(o[fin] - ro[fin]).max() <= 2.0 ** -6 * 4
+    l = lse.double().cpu().numpy()
+    assert np.array_equal(np.isfinite(l), np.isfinite(rl))
+
+
+def test_replays_of_a_captured_step(E):
+    """Append and attention captured once and replayed with other rows, positions and
+    tables, the eager twin's work in between: the same bits each time."""
+    x, y = Case(E, *SMALL, seed=11), Case(E, *SMALL, seed=11)
+    x.step([60, 33, 50]), y.step([60, 33, 50])
+    (q, k, v), _ = x.rows(9)
+    rope = torch.from_numpy(x.rope).cuda()
+    tab, rs, p0 = i32(x.table), i32([0, 2, 5, 9]), i32(x.len)
+    qo, out = torch.empty_like(q.contiguous()), torch.empty_like(q.contiguous())
+    ws = E.paged_attention_workspace(x.cache, 3, 9, 8, 5, 128)
+
+    def step(c, tab, rs, p0, q, k, v, qo, out, ws):
+        E.paged_append(c.cache, tab, rs, p0, k, v, q=q, rope=rope, q_out=qo, max_rows=5)
+        E.paged_attention(c.cache, tab, rs, p0, qo, out=out, workspace=ws, max_rows=5, max_len=128)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):  # also: another stream than the tensors' own
+        step(x, tab, rs, p0, q, k, v, qo, out, ws)
+    s.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(x, tab, rs, p0, q, k, v, qo, out, ws)
+    step(y, tab, rs, p0, q, k, v, torch.empty_like(qo), torch.empty_like(qo),
+         torch.empty_like(ws))
+    at, n = x.len.copy(), [[0, 2, 5, 9], [0, 5, 6, 9], [0, 0, 4, 8], [0, 3, 6, 9]]
+    for i in range(4):
+        (q2, k2, v2), _ = x.rows(9, 1.0 + i)
+        q.copy_(q2), k.copy_(k2), v.copy_(v2)
+        rs.copy_(i32(n[i])), p0.copy_(i32(at))
+        out.fill_(7.0)
+        g.replay()
+        q3, o3 = torch.empty_like(qo), torch.full_like(out, 7.0)
+        step(y, tab, rs, p0, q2, k2, v2, q3, o3, torch.empty_like(ws))
+        torch.cuda.synchronize()
+        m = n[i][-1]
+        assert torch.equal(qo[:m], q3[:m]) and torch.equal(out, o3)
+        for b in range(3):
+            for p in range(int(at[b]), int(at[b]) + n[i][b + 1] - n[i][b]):
+                x.plain.known[x.table[b, p // 32], p % 32] = True
+        kx, vx = values(x.cache)
+        ky, vy = values(y.cache)
+        for pg, sl in zip(*np.nonzero(x.plain.known)):
+            assert np.array_equal(kx[pg, :, sl], ky[pg, :, sl])
+            assert np.array_equal(vx[pg, :, sl], vy[pg, :, sl])
+        at = at + np.diff(n[i])
+
+
+def test_cache_past_32_bit_offsets(E):
+    """Pages beyond 4 GiB of codes: 8 heads of 128, pages of 1024."""
+    n = 4200  # pages of 1 MiB of keys
+    c = E.PagedCache(n, 1024, 8, 128, "e4m3", 64)
+    rng = np.random.RandomState(12)
+    table = np.array([[4199, 3], [2100, 4150]], np.int32)
+    x = Case.__new__(Case)
+    x.rng, x.hq, x.hkv, x.hd, x.dt = rng, 8, 8, 128, torch.bfloat16
+    (q, k, v), (fq, fk, fv) = x.rows(1100 + 30)
+    start, pos0 = [0, 1100, 1130], [0, 1010]
+    E.paged_append(c, i32(table), i32(start), i32(pos0), k, v)
+    out = E.paged_attention(c, i32(table), i32([0, 1, 2]), i32([1099, 1039]), q[[1099, 1129]].contiguous())
+    for b in range(2):
+        lo, m = (0, 1100) if b == 0 else (1010, 1040)
+        kk, vv = np.zeros((m, 8, 128)), np.zeros((m, 8, 128))
+        kk[lo:], vv[lo:] = fk[start[b]:start[b + 1]], fv[start[b]:start[b + 1]]
+        for h in range(8):
+            s = kk[:, h] @ fq[[1099, 1129][b], h] * 128 ** -0.5
+            w = np.exp(s - s.max())
+            ref = w @ vv[:, h] / w.sum()
+            # half a step of the codes moves scores (of std 1) and values by 2^-4
+            assert np.linalg.norm(out[b, h].double().cpu().numpy() - ref) <= 0.1 * np.linalg.norm(ref) + 0.02
+
+
+def test_table_rows_of_a_wider_table_and_strided_rows(E):
+    x = Case(E, *SMALL, seed=13)
+    x.step([60, 33, 50])
+    wide = torch.full((3, 9), -1, dtype=torch.int32, device="cuda")
+    wide[:, 2:6] = i32(x.table)
+    (q, k, v), _ = x.rows(4)
+    pad = torch.zeros(4, 8 * 128 + 64, dtype=torch.bfloat16, device="cuda")
+    out = pad[:, 32:32 + 1024].view(4, 8, 128)
+    rs, p0 = i32([0, 1, 2, 4]), i32(x.len)
+    E.paged_append(x.cache, wide[:, 2:6], rs, p0, k, v)
+    E.paged_attention(x.cache, wide[:, 2:6], rs, p0, q, out=out)
+    ref = E.paged_attention(x.cache, i32(x.table), rs, p0, q.contiguous())
+    assert torch.equal(out, ref) and bool((pad[:, :32] == 0).all()) and bool((pad[:, 1056:] == 0).all())
+    for bad in (lambda: E.paged_attention(x.cache, wide[:, 2:6].t(), rs, p0, q),
+                lambda: E.paged_attention(x.cache, i32(x.table), rs.long(), p0, q),
+                lambda: E.paged_attention(x.cache, i32(x.table), rs, p0, q.transpose(1, 2)),
+                lambda: E.paged_append(x.cache, i32(x.table), rs, p0, k, v.float()),
+                lambda: E.paged_append(x.cache, i32(x.table), rs, p0.cpu(), k, v)):
+        with pytest.raises(ValueError):
+            bad()
