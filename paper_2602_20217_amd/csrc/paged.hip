@@ -9,10 +9,11 @@
 //   values  [n_pages][hkv][page / 16][hd][16]   dimension-major in granules of 16 tokens
 //   scales  [n_pages][hkv][page / block]
 //
-// Both layouts are what the matrix instructions of the attention take: a 16x16x32
-// product reads 8 consecutive contraction elements per lane, which are dimensions
-// of one key in S = K Q^T and tokens of one dimension in O^T = V^T P^T, so keys and
-// values go from memory to operand registers with 16-byte loads and no transpose.
+// A 16x16x32 matrix instruction reads 8 consecutive contraction elements per lane:
+// dimensions of one key in S = K Q^T, tokens of one dimension in O^T = V^T P^T.  The
+// value layout is that operand as it stands (16 lanes read 256 contiguous bytes), so
+// values go from memory to operand registers; keys, whose rows lie on different
+// lanes, pass through LDS.
 //
 // A power of two as scale costs e4m3 nothing (its relative step does not depend on
 // the scale) and makes every change of scale exact but for codes that reach the
@@ -25,6 +26,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 namespace ks {
 
@@ -297,20 +299,30 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
 // ---------------------------------------------------------------- attention
 constexpr int DEC_NW = 4;       // waves of a split workgroup
 constexpr int KT = 64;          // keys of a tile
-constexpr int SPAN_MAX = 16384; // positions of a split (its page ids lie in LDS)
 
-// One wave's operand registers of a tile: 64 keys, 64 values.  Key row i of
-// subtile kt is key 16 (i / 4) + 4 kt + i % 4 of the tile, so lane group g of the
-// score registers holds the 16 consecutive keys from 16 g: one granule of values.
-//  keys    lane (i, g), i = lane % 16: row i of each subtile.  e4m3: 16 dims
-//          from 64 j + 16 g; bf16: 8 dims from 32 j + 8 g
+// One wave's tile in flight: 64 keys, 64 values.  Key row i of subtile kt is key
+// 16 (i / 4) + 4 kt + i % 4 of the tile, so lane group g of the score registers holds
+// the 16 consecutive keys from 16 g: one granule of values.
+//  keys    as they lie in memory: register u, lane l has bytes 1024 u + 16 l of the
+//          tile's rows.  (Loaded as operands instead, every lane of a quad another
+//          row, the loads took four times the cache accesses and held the kernel
+//          at 4.4 TB/s whatever the occupancy.)
 //  values  lane (i, g): dim 16 db + i, tokens 16 g..16 g + 15
 template <int HD, bool E4>
 struct Tile {
-  static constexpr int KJ = E4 ? HD / 64 : HD / 32;
+  static constexpr int RB = E4 ? HD : 2 * HD;  // bytes of a key row
+  static constexpr int CH = RB / 16;           // its 16-byte chunks
+  static constexpr int KU = KT * RB / 1024;    // key registers
+  static constexpr int PG = KU / 4;            // of them per granule of 16 keys
   static constexpr int VJ = E4 ? 1 : 2;
-  u32x4 k[4][KJ];
+  u32x4 k[KU];
   u32x4 v[HD / 16][VJ];
+  // Where chunk c of key row r lies in LDS: 8 lanes of an operand read have rows
+  // 4 kt + 0..3 and those 16 up, so these bits decide the bank.
+  __device__ static int at(int r, int c) {
+    const int f = CH == 4 ? ((r >> 1) & 1) | ((r >> 4) & 1) << 1 : (r & 3) | ((r >> 4) & 1) << 2;
+    return r * RB + ((c ^ f) << 4);
+  }
 };
 
 // 8 codes of two words as bf16, times the scale (exact)
@@ -342,9 +354,12 @@ __device__ inline void planes_of(float x, __bf16 (&o)[N]) {
       o[n] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(r) >> 16));  // towards 0
     else
       o[n] = (__bf16)r;
-    r -= (float)o[n];
-    if (n > 0 && x != 0.f && (float)o[n] == 0.f)
-      o[n] = (__bf16)copysignf(1.17549435e-38f, x);
+    const float y = (float)o[n];
+    r -= y;
+    if (n > 0) {  // |y| at least the smaller of |x| and 2^-126
+      const float z = fmaxf(fabsf(y), fminf(fabsf(x), 1.17549435e-38f));
+      o[n] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(copysignf(z, x)) >> 16));
+    }
   }
 }
 
@@ -371,23 +386,33 @@ __device__ inline uint32_t bytes_below(int n) {  // mask of the first n of 4 byt
   return n >= 4 ? ~0u : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
 }
 
+// Workgroups of a CU that the registers are cut for.  Two hide the start of one and
+// the joining of its waves behind the other; where that would spill (two column
+// blocks of head dim 128, three planes of queries against bf16) one is faster: 8 rows
+// of 64 sequences of 8192 tokens 240 us, 289 with spills.  Three spill everywhere.
+constexpr int dec_wgs(int HD, bool E4, int QP, int CB) {
+  return (CB == 1 || HD == 64) && (E4 || QP < 3) ? 2 : 1;
+}
+
 // Few rows.  A workgroup of four waves owns one split of `span` positions of one
 // kv head of one sequence and 16 CB of its query columns (column c: row c / G,
 // query head c % G of the kv head); wave w takes the split's tiles w, w + 4, ...
-// and runs a softmax with a running maximum and sum over them.  Keys are
-// requested again as soon as the scores are computed and values as soon as they
-// are added, so a tile's loads are in flight during the arithmetic of the one
-// before.  The four results meet in LDS, in wave order.
+// and runs a softmax with a running maximum and sum over them.  The next keys are
+// requested when these have gone to LDS and the next values when these are added,
+// so a tile's loads are in flight during the arithmetic of the one before.  The four results meet in LDS, in wave order.
 //
 // A column's arithmetic depends on its own query and length and on the split
 // only, never on the other columns or on CB.
+//
+// Memory bounds it: 64 sequences of 7700 tokens at 5.4 TB/s of cache, 512 of 8192 at
+// 5.8, with the arithmetic left out 5.7 and 6.2 (a plain stream of that size 7.0).
 //
 // Masked places: a key past a column's length is masked in the scores, whatever
 // it holds; a value there meets probability 0, so it must not be infinite or
 // NaN: values past the longest length are zeroed, and where those between the
 // shortest and the longest length hold one, the rows are added one at a time.
 template <int HD, bool E4, int QP, int CB>
-__global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
+__global__ __launch_bounds__(64 * DEC_NW, dec_wgs(HD, E4, QP, CB)) void k_pg_dec(PagedAttn a) {
   constexpr int PP = QP == 3 ? 3 : 1;  // probability planes
   constexpr int NS = HD / 32;          // contraction steps of a score
   constexpr int ND = HD / 16;          // blocks of 16 output dims
@@ -401,12 +426,18 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
   const int i16 = lane & 15, g = lane >> 4;
 
   int id = blockIdx.x;
-  const int split = id % a.nsplit;
-  id /= a.nsplit;
   const int kvh = id % c.hkv;
   id /= c.hkv;
   const int col0 = id % a.cblocks * 16 * CB;
-  const int b = id / a.cblocks;
+  id /= a.cblocks;
+  const int b = id % a.rows.B, split = id / a.rows.B;
+  const int start = split * a.span;
+  // the split's page ids, requested before the lengths say how many are needed
+  const int* tab = a.rows.table + (size_t)b * a.rows.table_ld + (start >> c.lpage);
+  const int np_most =
+      ((min(start + a.span, a.rows.max_len) - 1) >> c.lpage) - (start >> c.lpage) + 1;
+  int pid0 = 0;
+  if ((int)threadIdx.x < np_most) pid0 = tab[threadIdx.x];
   const SeqRows sr = seq_rows(a.rows, b);
   if (a.rows.err && threadIdx.x == 0 && sr.over) a.rows.err[b] = 1;
   const int ncol = min(sr.n * G - col0, 16 * CB);
@@ -432,30 +463,34 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
   lmin = __builtin_amdgcn_readfirstlane(lmin);
   lmax = __builtin_amdgcn_readfirstlane(lmax);
   if (a.rows.err && over) a.rows.err[b] = 1;
-  const int start = split * a.span;
   const int stop = min(lmax, start + a.span);
   if (start >= stop && split > 0) return;  // no partial is read from here
 
   // the split's page ids
   int* s_page = (int*)smem;
   const int np = stop > start ? ((stop - 1) >> c.lpage) - (start >> c.lpage) + 1 : 0;
-  for (int i = threadIdx.x; i < np; i += 64 * DEC_NW) {
-    const int pid = a.rows.table[(size_t)b * a.rows.table_ld + (start >> c.lpage) + i];
+  bool lost = false;
+  for (int i0 = 0; i0 < np; i0 += 64 * DEC_NW) {  // the last id again by who has none left
+    const int i = min(i0 + (int)threadIdx.x, np - 1);
+    const int pid = i0 == 0 && (int)threadIdx.x < np ? pid0 : tab[i];
     const bool ok = pid >= 0 && pid < c.n_pages;
     s_page[i] = ok ? pid : -1;
-    if (!ok && a.rows.err) a.rows.err[b] = 1;
+    lost |= !ok;
   }
+  if (a.rows.err && __any(lost)) a.rows.err[b] = 1;
 
-  // query columns
-  bf16x8 q[CB][NS][QP];
+  // the query columns' operands, in LDS for all waves: block (cb, step, plane), 16
+  // bytes a lane
+  bf16x8* s_q = (bf16x8*)(smem + a.lds_pages);
   const size_t es = QP == 1 ? 2 : 4;
-#pragma unroll
-  for (int cb = 0; cb < CB; ++cb) {
-    const int cc = col0 + min(16 * cb + i16, ncol - 1);
+  for (int x = w; x < CB * NS; x += DEC_NW) {
+    const int cc = col0 + min(16 * (x / NS) + i16, ncol - 1);
     const char* p = (const char*)a.q +
                     ((size_t)(sr.r0 + cc / G) * a.ldq + (size_t)(kvh * G + cc % G) * HD) * es;
+    bf16x8 y[QP];
+    load_q<QP>(p + dim_of<E4>(x % NS, g) * es, QP != 1, y);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) load_q<QP>(p + dim_of<E4>(s, g) * es, QP != 1, q[cb][s]);
+    for (int n = 0; n < QP; ++n) s_q[(x * QP + n) * 64 + lane] = y[n];
   }
   __syncthreads();
 
@@ -477,66 +512,83 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
     if (pid < 0) return -1;
     return (((long long)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1));
   };
-  const size_t eb = E4 ? 1 : 2;
-  auto load_k = [&](TileT& t, float& ks, int t0) {
-    const long long tok = max(granule(t0, i16 >> 2), 0ll);
-    const char* p = (const char*)c.k + ((size_t)tok + (i16 & 3)) * HD * eb + 16 * g;
+  // Loads of places that hold no token (past the end, invalid pages) read the
+  // cache's first page; what they bring is masked.
+  constexpr size_t eb = E4 ? 1 : 2;
+  auto load_k = [&](TileT& t, int t0) {
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt)
+    for (int gr = 0; gr < 4; ++gr) {
+      const long long tok = max(granule(t0, gr), 0ll);
+      const int hi = __builtin_amdgcn_readfirstlane((int)(tok >> 32));
+      const uint32_t lo = __builtin_amdgcn_readfirstlane((int)tok);
+      const char* p = (const char*)c.k + (((size_t)hi << 32) | lo) * TileT::RB;
 #pragma unroll
-      for (int j = 0; j < TileT::KJ; ++j)
-        t.k[kt][j] = *(const u32x4*)(p + (size_t)(4 * kt) * HD * eb + 64 * j);
-    if (E4) ks = c.k_scale[(size_t)(tok >> c.lblock)];
+      for (int u = 0; u < TileT::PG; ++u)
+        t.k[gr * TileT::PG + u] = *(const u32x4*)(p + 1024 * u + 16 * lane);
+    }
   };
-  auto load_v = [&](TileT& t, float& vs, int t0) {
-    const long long tok = granule(t0, g);
+  auto load_v = [&](TileT& t, long long tok) {
     const char* p = (const char*)c.v + ((size_t)max(tok, 0ll) * HD + (size_t)i16 * GRAN) * eb;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int j = 0; j < TileT::VJ; ++j)
         t.v[d][j] = *(const u32x4*)(p + (size_t)(16 * d) * GRAN * eb + 16 * j);
-    if (E4) vs = tok < 0 ? 1.f : c.v_scale[(size_t)(tok >> c.lblock)];
+  };
+  auto load_s = [&](float& ks, float& vs, long long tok) {
+    if (!E4) return;
+    ks = c.k_scale[(size_t)(max(tok, 0ll) >> c.lblock)];
+    vs = c.v_scale[(size_t)(max(tok, 0ll) >> c.lblock)];
   };
 
   const float sc = a.scale * LOG2E;
+  unsigned char* kb =  // this wave's keys
+      smem + a.lds_pages + CB * NS * QP * 1024 + w * (KT * TileT::RB);
   TileT t;
-  float ks = 1.f, vs = 1.f;
-  int t0 = start + w * KT;
-  if (t0 < stop) {
-    load_k(t, ks, t0);
-    load_v(t, vs, t0);
-  }
-  for (; t0 < stop; t0 += DEC_NW * KT) {
-    const int tn = t0 + DEC_NW * KT;
+  auto stage = [&]() {
+#pragma unroll
+    for (int u = 0; u < TileT::KU; ++u)
+      *(u32x4*)(kb + TileT::at((64 / TileT::CH) * u + lane / TileT::CH, lane % TileT::CH)) = t.k[u];
+  };
+  // One tile whose keys lie in LDS and whose values are in flight.  MASK: some of its
+  // keys are past a column's length or on an invalid page.  Both forms compute the
+  // same bits of what is not masked.
+  auto tile = [&](auto mask_, int t0, bool have, float ksc, float vsc) {
+#pragma clang fp contract(off)
+    constexpr bool MASK = decltype(mask_)::value;
     // scores: row 4 g + v of subtile kt is key 16 g + 4 kt + v, column lane % 16
     f32x4 s[CB][4];
 #pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
+    for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-      for (int cb = 0; cb < CB; ++cb) s[cb][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < 4; ++kt) s[cb][kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int row = 16 * (i16 >> 2) + (i16 & 3);
+    u32x4 x[4];
 #pragma unroll
-      for (int st = 0; st < NS; ++st) {
-        bf16x8 kk;
-        if (E4) {
-          const u32x4 x = t.k[kt][st >> 1];
-          kk = (st & 1) ? widen(x[2], x[3], ks) : widen(x[0], x[1], ks);
-        } else {
-          kk = __builtin_bit_cast(bf16x8, t.k[kt][st]);
-        }
+    for (int st = 0; st < NS; ++st) {
+      if (!E4 || (st & 1) == 0)
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt)
+          x[kt] = *(const u32x4*)(kb + TileT::at(row + 4 * kt, (E4 ? 2 : 4) * st + g));
+      bf16x8 qq[CB][QP];
+#pragma unroll
+      for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+        for (int n = 0; n < QP; ++n) qq[cb][n] = s_q[((cb * NS + st) * QP + n) * 64 + lane];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const bf16x8 kk = !E4        ? __builtin_bit_cast(bf16x8, x[kt])
+                          : (st & 1) ? widen(x[kt][2], x[kt][3], 1.f)
+                                     : widen(x[kt][0], x[kt][1], 1.f);
 #pragma unroll
         for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
           for (int n = 0; n < QP; ++n)
-            s[cb][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, q[cb][st][n], s[cb][kt], 0, 0, 0);
+            s[cb][kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kk, qq[cb][n], s[cb][kt], 0, 0, 0);
       }
+      if (CB > 1) __builtin_amdgcn_sched_barrier(0);  // keeps operands from piling up
     }
-    const bool have = granule(t0, g) >= 0;  // this lane group's keys
-    float ksn = 1.f, vsn = 1.f;
-    if (tn < stop) load_k(t, ksn, tn);
-
     // softmax step
-    const bool ragged = t0 + KT > lmin || __any(!have);
     bf16x8 p[CB][2][PP];
 #pragma unroll
     for (int cb = 0; cb < CB; ++cb) {
@@ -545,16 +597,21 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
       for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-          float x = s[cb][kt][v] * sc;
-          if (ragged && !(have && t0 + 16 * g + 4 * kt + v < len[cb])) x = -INFINITY;
+          float x = s[cb][kt][v] * ksc;
+          if (MASK && !(have && t0 + 16 * g + 4 * kt + v < len[cb])) x = -INFINITY;
           s[cb][kt][v] = x;
           mx = fmaxf(mx, x);
         }
       mx = fmaxf(mx, __shfl_xor(mx, 16));
       mx = fmaxf(mx, __shfl_xor(mx, 32));
       const float mn = fmaxf(m[cb], mx);
-      const float al = __builtin_amdgcn_exp2f(m[cb] - mn);
-      m[cb] = mn;
+      if (__any(mn != m[cb])) {  // otherwise the factor is 1
+        const float al = __builtin_amdgcn_exp2f(m[cb] - mn);
+        m[cb] = mn;
+        l[cb] *= al;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[cb][d] *= al;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int kt = 0; kt < 4; ++kt)
@@ -569,19 +626,29 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
 #pragma unroll
           for (int n = 0; n < PP; ++n) p[cb][kt >> 1][n][4 * (kt & 1) + v] = y[n];
         }
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
-      l[cb] = l[cb] * al + sum;
-#pragma unroll
-      for (int d = 0; d < ND; ++d) o[cb][d] *= al;
+      l[cb] += sum;  // of this lane group's keys
+      if (CB > 1) __builtin_amdgcn_sched_barrier(0);
     }
-
     // values
-    bool slow = false;
-    if (ragged) {
-      // this lane group's tokens below the longest and below the shortest length
-      const int hi = have ? min(lmax - (t0 + GRAN * g), GRAN) : 0;
-      const int lo = have ? min(lmin - (t0 + GRAN * g), GRAN) : 0;
+    auto operand = [&](int d, int st, int upto) {  // tokens from `upto` on as 0
+      if (E4) {
+        uint32_t w0 = t.v[d][0][2 * st], w1 = t.v[d][0][2 * st + 1];
+        if (MASK) {
+          w0 &= bytes_below(upto - 8 * st);
+          w1 &= bytes_below(upto - 8 * st - 4);
+        }
+        return widen(w0, w1, vsc);
+      }
+      u32x4 x = t.v[d][TileT::VJ == 2 ? st : 0];
+      if (MASK)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) x[y] &= bytes_below(2 * (upto - 8 * st - 2 * y));
+      return __builtin_bit_cast(bf16x8, x);
+    };
+    // this lane group's tokens below the longest and below the shortest length
+    const int upto = MASK && have ? min(lmax - (t0 + GRAN * g), GRAN) : 0;
+    if (MASK) {
+      const int from = have ? min(lmin - (t0 + GRAN * g), GRAN) : 0;
       uint32_t odd = 0;  // an infinite or NaN value between the two
 #pragma unroll
       for (int d = 0; d < ND; ++d)
@@ -590,79 +657,99 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
             if (E4) {
-              const uint32_t in = bytes_below(hi - 4 * x);
-              const uint32_t y = t.v[d][j][x] & in;
-              t.v[d][j][x] = y;
-              odd |= ((y & 0x7F7F7F7Fu & ~bytes_below(lo - 4 * x)) + 0x01010101u) & 0x80808080u;
+              const uint32_t in = bytes_below(upto - 4 * x) & ~bytes_below(from - 4 * x);
+              odd |= ((t.v[d][j][x] & 0x7F7F7F7Fu & in) + 0x01010101u) & 0x80808080u;
             } else {
               const int at = 8 * j + 2 * x;
-              const uint32_t in = bytes_below(2 * (hi - at));
-              const uint32_t y = t.v[d][j][x] & in;
-              t.v[d][j][x] = y;
-              const uint32_t z = y & 0x7FFF7FFFu & ~bytes_below(2 * (lo - at));
+              const uint32_t in = bytes_below(2 * (upto - at)) & ~bytes_below(2 * (from - at));
+              const uint32_t z = t.v[d][j][x] & 0x7FFF7FFFu & in;
               odd |= (z & 0xFFFFu) >= 0x7F80u || (z >> 16) >= 0x7F80u;
             }
           }
-      slow = __any(odd != 0);
-    }
-    if (!slow) {
+      if (__any(odd != 0)) {  // row by row, every one with its own length
+        for (int r = col0 / G; r <= (col0 + ncol - 1) / G; ++r) {
+          const int rl = row_len(a, sr, b, r, over);
+          const int mine = have ? min(rl - (t0 + GRAN * g), GRAN) : 0;
 #pragma unroll
-      for (int d = 0; d < ND; ++d)
+          for (int d = 0; d < ND; ++d) {
+            f32x4 add[CB];
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          bf16x8 vv;
-          if (E4)
-            vv = st ? widen(t.v[d][0][2], t.v[d][0][3], vs) : widen(t.v[d][0][0], t.v[d][0][1], vs);
-          else
-            vv = __builtin_bit_cast(bf16x8, t.v[d][TileT::VJ == 2 ? st : 0]);
+            for (int cb = 0; cb < CB; ++cb) add[cb] = o[cb][d];
 #pragma unroll
-          for (int cb = 0; cb < CB; ++cb)
+            for (int st = 0; st < 2; ++st) {
+              const bf16x8 vv = operand(d, st, mine);
 #pragma unroll
-            for (int n = 0; n < PP; ++n)
-              o[cb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], o[cb][d], 0, 0, 0);
-        }
-    } else {
-      for (int r = col0 / G; r <= (col0 + ncol - 1) / G; ++r) {
-        // the row's own length, and its tokens of this lane group
-        const int rl = row_len(a, sr, b, r, over);
-        const int hi = have ? min(rl - (t0 + GRAN * g), GRAN) : 0;
+              for (int cb = 0; cb < CB; ++cb)
 #pragma unroll
-        for (int d = 0; d < ND; ++d) {
-          f32x4 add[CB];
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb) add[cb] = o[cb][d];
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            bf16x8 vv;
-            if (E4) {
-              const uint32_t w0 = t.v[d][0][2 * st] & bytes_below(hi - 8 * st);
-              const uint32_t w1 = t.v[d][0][2 * st + 1] & bytes_below(hi - 8 * st - 4);
-              vv = widen(w0, w1, vs);
-            } else {
-              u32x4 x = t.v[d][TileT::VJ == 2 ? st : 0];
-#pragma unroll
-              for (int y = 0; y < 4; ++y) x[y] &= bytes_below(2 * (hi - 8 * st - 2 * y));
-              vv = __builtin_bit_cast(bf16x8, x);
+                for (int n = 0; n < PP; ++n)
+                  add[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], add[cb], 0, 0, 0);
             }
 #pragma unroll
             for (int cb = 0; cb < CB; ++cb)
-#pragma unroll
-              for (int n = 0; n < PP; ++n)
-                add[cb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], add[cb], 0, 0, 0);
+              if ((col0 + 16 * cb + i16) / G == r) o[cb][d] = add[cb];
           }
-#pragma unroll
-          for (int cb = 0; cb < CB; ++cb)
-            if ((col0 + 16 * cb + i16) / G == r) o[cb][d] = add[cb];
         }
+        return;
       }
     }
-    if (tn < stop) load_v(t, vsn, tn);
-    ks = ksn;
-    vs = vsn;
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+#pragma unroll
+      for (int st = 0; st < 2; ++st) {
+        const bf16x8 vv = operand(d, st, upto);
+#pragma unroll
+        for (int cb = 0; cb < CB; ++cb)
+#pragma unroll
+          for (int n = 0; n < PP; ++n)
+            o[cb][d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[cb][st][n], o[cb][d], 0, 0, 0);
+      }
+      if (CB > 1 && (d & 1)) __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  // tiles that every column attends whole, each one's loads in flight during the
+  // arithmetic of the one before; then the others
+  constexpr int STEP = DEC_NW * KT;
+  const int whole = min(stop, lmin);
+  int t0 = start + w * KT;
+  bool bad = false;  // an invalid page among them
+  float ks = 1.f, vs = 1.f;
+  if (t0 + KT <= whole) {
+    long long tok = granule(t0, g);  // of this lane group's keys and values
+    load_k(t, t0);
+    load_s(ks, vs, tok);
+    load_v(t, tok);
+    for (; t0 + KT <= whole; t0 += STEP) {
+      const bool ok = __all(tok >= 0);
+      const float ksc = ks * sc, vsc = vs;
+      stage();
+      tok = granule(t0 + STEP, g);
+      load_k(t, t0 + STEP);
+      load_s(ks, vs, tok);
+      if (ok) tile(std::false_type{}, t0, true, ksc, vsc);
+      bad |= !ok;
+      load_v(t, tok);
+    }
+  }
+  if (bad) t0 = start + w * KT;
+  for (; t0 < stop; t0 += STEP) {
+    const long long tok = granule(t0, g);
+    const bool have = tok >= 0;
+    if (t0 + KT <= whole && __all(have)) continue;
+    load_k(t, t0);
+    load_s(ks, vs, tok);
+    load_v(t, tok);
+    stage();
+    tile(std::true_type{}, t0, have, ks * sc, have ? vs : 1.f);
+  }
+#pragma unroll
+  for (int cb = 0; cb < CB; ++cb) {
+    l[cb] += __shfl_xor(l[cb], 16);
+    l[cb] += __shfl_xor(l[cb], 32);
   }
 
   // merge of the waves: record of wave w, column cc at (w 16 CB + cc) RS
-  __syncthreads();  // the page ids are no longer read
+  __syncthreads();  // the page ids and keys are no longer read
   float* rec = (float*)smem;
 #pragma unroll
   for (int cb = 0; cb < CB; ++cb) {
@@ -715,45 +802,50 @@ __global__ __launch_bounds__(64 * DEC_NW) void k_pg_dec(PagedAttn a) {
   }
 }
 
-// One wave per (row, query head): joins the splits that hold keys of the row, in
-// order.  Partials are (o[hd], max, sum) with the maximum in natural units.
-template <typename T, int HD>
+// NW waves per (row, query head) join the splits that hold keys of the row, each of
+// them every NW-th, in order, then the waves' results.  Partials are (o[hd], max,
+// sum) with the maximum in natural units.  The first partials are requested before
+// the row's length is known (what they hold then is not used), so the loads of a
+// launch lie one memory latency deep, not three: 32 splits of one row's 32 heads 4.0 us
+// with four waves, 12.2 with one that asks for the length first.
+template <typename T, int HD, int NW>
 __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
   constexpr int DPL = HD / 64;
-  const int lane = threadIdx.x & 63;
-  const int job = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int r = job / a.hq, h = job % a.hq;
-  if (r >= a.rows.rows) return;
-  const int b = seq_of(a.rows, r);
-  if (b < 0) return;
-  const SeqRows sr = seq_rows(a.rows, b);
-  if (r - sr.r0 >= sr.n || sr.n * (a.hq / a.cache.hkv) > a.col_max) return;
-  bool over = false;
-  const int n = row_len(a, sr, b, r - sr.r0, over);
-  const int ns = (n + a.span - 1) / a.span;
+  constexpr int U = 8;
+  __shared__ float s_o[4][HD], s_m[4], s_l[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % NW;
+  const int job = blockIdx.x * (4 / NW) + wave / NW;
+  const int r = min(job / a.hq, a.rows.rows - 1), h = job % a.hq;
   const float* p = a.part + ((size_t)r * a.hq + h) * a.nsplit_ld * (HD + 2);
+  float ms[U], ls[U], ov[U][DPL];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      const float* x = p + (size_t)min(s0 + NW * k, a.nsplit - 1) * (HD + 2);
+      ms[k] = x[HD];
+      ls[k] = x[HD + 1];
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) ov[k][e] = x[DPL * lane + e];
+    }
+  };
+  load(w);
+  const int b = seq_of(a.rows, r);
+  int ns = 0;
+  bool mine = job < a.rows.rows * a.hq && b >= 0;
+  if (mine) {
+    const SeqRows sr = seq_rows(a.rows, b);
+    mine = r - sr.r0 < sr.n && sr.n * (a.hq / a.cache.hkv) <= a.col_max;
+    bool over = false;
+    ns = (row_len(a, sr, b, r - sr.r0, over) + a.span - 1) / a.span;
+  }
   float m = -FLT_MAX, l = 0.f, o[DPL];
 #pragma unroll
   for (int e = 0; e < DPL; ++e) o[e] = 0.f;
-  constexpr int U = 8;
-  for (int s0 = 0; s0 < ns; s0 += U) {
-    float ms[U], ls[U], ov[U][DPL];
+  for (int s0 = w; s0 < ns; s0 += NW * U) {
+    if (s0 != w) load(s0);
 #pragma unroll
     for (int k = 0; k < U; ++k) {
-      ms[k] = -FLT_MAX;
-      ls[k] = 0.f;
-#pragma unroll
-      for (int e = 0; e < DPL; ++e) ov[k][e] = 0.f;
-      if (s0 + k < ns) {
-        const float* x = p + (size_t)(s0 + k) * (HD + 2);
-        ms[k] = x[HD];
-        ls[k] = x[HD + 1];
-#pragma unroll
-        for (int e = 0; e < DPL; ++e) ov[k][e] = x[DPL * lane + e];
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < U; ++k) {
+      if (s0 + NW * k >= ns) break;
       const float mn = fmaxf(m, ms[k]);
       const float ea = __expf(m - mn), eb = __expf(ms[k] - mn);
       l = fmaf(ls[k], eb, l * ea);
@@ -762,6 +854,28 @@ __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
       m = mn;
     }
   }
+  if (NW > 1) {
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) s_o[wave][DPL * lane + e] = o[e];
+    if (lane == 0) {
+      s_m[wave] = m;
+      s_l[wave] = l;
+    }
+    __syncthreads();
+    if (w != 0) return;
+    m = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    l = 0.f;
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) {
+      const float f = __expf(s_m[k] - m);
+      l = fmaf(s_l[k], f, l);
+#pragma unroll
+      for (int e = 0; e < DPL; ++e) o[e] = fmaf(s_o[k][DPL * lane + e], f, o[e]);
+    }
+  }
+  if (!mine) return;
   T* dst = (T*)a.out + (size_t)r * a.ldo + (size_t)h * HD + DPL * lane;
   const bool any = l != 0.f;
   const float inv = 1.0f / l;
@@ -795,11 +909,15 @@ void paged_append(const PagedAppend& a, hipStream_t st) {
 #undef KS_APP
 }
 
+// Splits: as many as give every CU a workgroup (one sequence of 32768 tokens: 17.8 us
+// with 256 workgroups, 21.1 with 384 and 27.5 with 1024, the rest being their start
+// and the merge), none shorter than a tile for every wave, and none longer than 4096
+// positions, which keeps sequences of different lengths level (64 of 500 to 15000
+// tokens: 216 us, 225 to 250 with one split each).
 int paged_splits(int B, int hkv, int G, int max_rows, int max_len) {
   const int blocks = B * hkv * ((max_rows * G + 31) / 32);
   const int most = std::max(1, (max_len + DEC_NW * KT - 1) / (DEC_NW * KT));
-  const int want = std::max((1024 + blocks - 1) / blocks, (max_len + SPAN_MAX - 1) / SPAN_MAX);
-  return std::min(want, most);
+  return std::min(std::max((255 + blocks) / blocks, (max_len + 4095) / 4096), most);
 }
 
 void paged_attention(const PagedAttn& a_, hipStream_t st) {
@@ -811,8 +929,11 @@ void paged_attention(const PagedAttn& a_, hipStream_t st) {
   const int CB = cols <= 16 ? 1 : 2;
   a.cblocks = (cols + 16 * CB - 1) / (16 * CB);
   const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
-  const int np = a.span / c.page + 2;
-  const size_t lds = std::max((size_t)DEC_NW * 16 * CB * (c.hd + 4) * 4, (size_t)np * 4);
+  a.lds_pages = (a.span / c.page + 2) * 4 + 15 & ~15;
+  const int planes = a.planes ? a.planes : a.dtype == KS_BF16 ? 1 : 3;
+  const size_t lds = std::max((size_t)DEC_NW * 16 * CB * (c.hd + 4) * 4,
+                              (size_t)a.lds_pages + CB * c.hd / 32 * planes * 1024 +
+                                  DEC_NW * KT * c.hd * (c.kind == KS_E4M3 ? 1 : 2));
 #define KS_DEC(HD_, E_, QP_)                                                              \
   do {                                                                                    \
     if (CB == 1) KS_LAUNCH((k_pg_dec<HD_, E_, QP_, 1>), grid, dim3(256), lds, st, a);     \
@@ -825,15 +946,20 @@ void paged_attention(const PagedAttn& a_, hipStream_t st) {
     else if (c.kind == KS_E4M3) KS_DEC(64, true, QP_);                 \
     else KS_DEC(64, false, QP_);                                       \
   } while (0)
-  const int planes = a.planes ? a.planes : a.dtype == KS_BF16 ? 1 : 3;
   if (planes == 1) KS_DEC_T(1);
   else if (planes == 2) KS_DEC_T(2);
   else KS_DEC_T(3);
 #undef KS_DEC_T
 #undef KS_DEC
   if (!a.part || !a.out) return;
-  const dim3 mgrid((unsigned)(((size_t)a.rows.rows * a.hq + 3) / 4));
-#define KS_MRG(T_, HD_) KS_LAUNCH((k_pg_merge<T_, HD_>), mgrid, dim3(256), 0, st, a)
+  // up to eight splits are one wave's loads
+  const int per = a.nsplit > 8 ? 1 : 4;  // (row, head) pairs of a workgroup
+  const dim3 mgrid((unsigned)(((size_t)a.rows.rows * a.hq + per - 1) / per));
+#define KS_MRG(T_, HD_)                                                                 \
+  do {                                                                                  \
+    if (per == 1) KS_LAUNCH((k_pg_merge<T_, HD_, 4>), mgrid, dim3(256), 0, st, a);      \
+    else KS_LAUNCH((k_pg_merge<T_, HD_, 1>), mgrid, dim3(256), 0, st, a);               \
+  } while (0)
   if (a.dtype == KS_BF16) {
     if (c.hd == 128) KS_MRG(bf16_t, 128);
     else KS_MRG(bf16_t, 64);

@@ -436,11 +436,13 @@ def _need(ok: bool, msg: str):
 
 def _here(dev: torch.device, f, *args):
     """Calls f with args and the current stream of dev, dev being current."""
-    if dev.index == torch.cuda.current_device():
-        f(*args, _stream())
+    i = dev.index
+    s = torch._C._cuda_getCurrentRawStream(i)  # current_stream() builds an object: 2.8 us
+    if i == torch.cuda.current_device():
+        f(*args, s)
     else:
         with torch.cuda.device(dev):
-            f(*args, _stream())
+            f(*args, s)
 
 
 _DT = {torch.float32: K.KS_F32, torch.bfloat16: K.KS_BF16}
@@ -448,10 +450,11 @@ _DT = {torch.float32: K.KS_F32, torch.bfloat16: K.KS_BF16}
 
 def _rows3(t: torch.Tensor, heads: int, hd: int, name: str) -> int:
     """Row stride (elements) of t [rows, heads, hd], dense inside a row."""
-    _need(t.dim() == 3 and t.shape[1] == heads and t.shape[2] == hd and
-          (t.shape[0] == 0 or t.stride(2) == 1 and (heads == 1 or t.stride(1) == hd)),
-          f"{name} must be [rows, {heads}, {hd}], dense rows")
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), heads * hd)
+    n, h, d = t.shape if t.dim() == 3 else (0, 0, 0)
+    ld, sh, sd = t.stride() if t.dim() == 3 else (0, 0, 0)
+    if h != heads or d != hd or n and (sd != 1 or heads != 1 and sh != hd):
+        raise ValueError(f"{name} must be [rows, {heads}, {hd}], dense rows")
+    return ld if n > 1 else max(ld, heads * hd)
 
 
 def sample_draw_workspace(rows: int, vocab: int, device="cuda") -> torch.Tensor:

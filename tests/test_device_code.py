@@ -63,3 +63,19 @@ def test_split_sums_take_rows_at_any_float_address(tmp_path):
         loads = re.findall(r"= load <4 x float>, ptr addrspace\(1\) %\S+, align (\d+)", body)
         resid = "ILi1E" in body.split("\n", 1)[0]  # EPI_RESID
         assert ("4" in loads) == resid, loads
+
+
+@pytest.mark.parametrize("src", ["paged.hip"])
+def test_no_scalar_register_spills(src, tmp_path):
+    """Scalar registers spilled to lanes of a vector register at the head of a block
+    make the compiler place copies of vector registers there before the block restores
+    its execution mask, so lanes lose them.  The kernels stay below that."""
+    if not os.path.exists(B.HIPCC):
+        pytest.skip("no hipcc")
+    flags = [f for f in B.FLAGS if f != "-fPIC"]
+    r = subprocess.run([B.HIPCC, *flags, "--cuda-device-only", "-S", os.path.join(B.CSRC, src),
+                        "-o", str(tmp_path / "device.s"),
+                        "-Rpass-analysis=kernel-resource-usage"], check=True,
+                       capture_output=True, text=True)
+    spills = re.findall(r"SGPRs Spill: (\d+)", r.stderr)
+    assert spills and set(spills) == {"0"}, spills
