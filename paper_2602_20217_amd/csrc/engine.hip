@@ -1241,7 +1241,10 @@ size_t ks_paged_attention_workspace_bytes(const ks_paged_cache* cache, int B, in
       hq < cache->hkv || hq % cache->hkv || max_rows < 1 || max_len < 1)
     return 0;
   if (B == 0 || rows == 0) return 256;
-  const int ns = ks::paged_splits(B, cache->hkv, hq / cache->hkv, std::min(max_rows, rows), max_len);
+  int ns = 1;  // of either dtype
+  for (int planes : {1, 3})
+    ns = std::max(ns, ks::paged_plan(B, cache->hkv, hq / cache->hkv, std::min(max_rows, rows),
+                                     max_len, planes).nsplit);
   return ns > 1 ? (size_t)rows * hq * ns * (cache->hd + 2) * 4 : 256;
 }
 
@@ -1264,7 +1267,9 @@ ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* r
       "rows of q and out must be 16-byte aligned");
   const int G = hq / cache->hkv;
   const int len = std::max(1, rows->max_len);
-  const int ns = ks::paged_splits(rows->B, cache->hkv, G, a.rows.max_rows, len);
+  const ks::PagedPlan plan =
+      ks::paged_plan(rows->B, cache->hkv, G, a.rows.max_rows, len, dtype == KS_BF16 ? 1 : 3);
+  const int ns = plan.nsplit;
   REQ((long long)ns * cache->hkv * ((long long)a.rows.max_rows * G / 16 + 1) * rows->B < (1ll << 31) &&
           (long long)rows->rows * hq < (1ll << 31),
       "too many rows and heads for one launch");
@@ -1285,7 +1290,7 @@ ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* r
   a.dtype = dtype;
   a.scale = scale;
   a.nsplit = a.nsplit_ld = ns;
-  a.span = ((len + ns - 1) / ns + 63) / 64 * 64;
+  a.span = plan.span;
   a.part = ns > 1 ? (float*)workspace : nullptr;
   ks::paged_attention(a, (hipStream_t)stream);
   HIPCHK(hipGetLastError());

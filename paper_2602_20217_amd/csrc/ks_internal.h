@@ -270,11 +270,15 @@ struct PagedAttn {
   // bf16 planes of queries: 1 (bf16), 3 (float32), or 2 with probabilities in one
   int planes = 0;    // 0: by dtype
   bool few = false;  // split kernel whatever the number of rows
-  int col_max = 0, cblocks = 0, lds_pages = 0;  // set by paged_attention
+  int col_max = 0, col_min = 0, cblocks = 0, lds_pages = 0;  // set by paged_attention
 };
 void paged_attention(const PagedAttn& a, hipStream_t st);
-// splits of a launch over at most max_rows rows a sequence and max_len positions
-int paged_splits(int B, int hkv, int G, int max_rows, int max_len);
+// Splits of a call over at most max_rows rows a sequence and max_len positions.
+struct PagedPlan {
+  bool chunk;  // the longest sequences go to the chunk kernel
+  int nsplit, span;
+};
+PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int planes);
 
 // ---------------------------------------------------- vocabulary reductions
 // argmax (lowest index on ties) and top-1 probability of each of M rows of V

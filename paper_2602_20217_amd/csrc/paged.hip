@@ -21,6 +21,7 @@
 //
 //  k_pg_append  new rows: rotation, scales, codes, and the rotated queries
 //  k_pg_dec     attention of few rows a sequence, split over the context
+//  k_pg_chunk   attention of many rows (prompt chunks)
 //  k_pg_merge   joins the splits of a row
 #include "ks_internal.h"
 
@@ -802,6 +803,400 @@ __global__ __launch_bounds__(64 * DEC_NW, dec_wgs(HD, E4, QP, CB)) void k_pg_dec
   }
 }
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// max over the two lanes l and l + 32, to both: the instruction swaps the upper half
+// of its first register with the lower half of the second
+__device__ inline float max_halves(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// One column by a wave, without matrix instructions: lanes take keys, then dims.  Only
+// what it attends is read.
+template <int HD, bool E4, int QP>
+__device__ __attribute__((noinline)) void column(const PagedAttn& a, const SeqRows& sr, int b,
+                                                 int kvh, int cc, int start, int stop, int split) {
+  constexpr int DPL = HD / 64;
+  const PagedCache& c = a.cache;
+  const int G = a.hq / c.hkv, lane = threadIdx.x & 63;
+  const int h = kvh * G + cc % G;
+  const size_t r = sr.r0 + cc / G;
+  bool over = false;
+  const int n = row_len(a, sr, b, cc / G, over);
+  if (a.part && n <= start) return;
+  const int* tab = a.rows.table + (size_t)b * a.rows.table_ld;
+  float m = -FLT_MAX, l = 0.f, o[DPL];
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) o[e] = 0.f;
+  auto qv = [&](int d) {
+    const size_t at = r * a.ldq + (size_t)h * HD + d;
+    return QP == 1 ? bf2f(((const bf16_t*)a.q)[at]) : ((const float*)a.q)[at];
+  };
+  auto cached = [&](const void* p, size_t at) {
+    return E4 ? value_of(((const uint8_t*)p)[at]) : bf2f(((const bf16_t*)p)[at]);
+  };
+  for (int t0 = start; t0 < min(stop, n); t0 += 64) {
+    const int p = min(t0 + lane, min(stop, n) - 1);
+    const int pid = tab[p >> c.lpage];
+    const bool ok = t0 + lane < min(stop, n) && pid >= 0 && pid < c.n_pages;
+    const size_t tok = ok ? (((size_t)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1)) : 0;
+    float s = 0.f;
+    for (int d = 0; d < HD; ++d) s = fmaf(qv(d), cached(c.k, tok * HD + d), s);
+    if (E4) s *= c.k_scale[tok >> c.lblock];
+    s = ok ? s * (a.scale * LOG2E) : -INFINITY;
+    const float mn = fmaxf(m, wave_max64(s));
+    const float al = __builtin_amdgcn_exp2f(m - mn), e = __builtin_amdgcn_exp2f(s - mn);
+    m = mn;
+    l = l * al + group_sum<64>(e);
+#pragma unroll
+    for (int x = 0; x < DPL; ++x) o[x] *= al;
+    for (int t = 0; t < 64; ++t) {
+      if (!__shfl((int)ok, t)) continue;
+      const float pt = __shfl(e, t);
+      const size_t tt = ((size_t)__shfl((int)(tok >> 32), t) << 32) | (uint32_t)__shfl((int)tok, t);
+      const float vsc = E4 ? c.v_scale[tt >> c.lblock] : 1.f;
+#pragma unroll
+      for (int x = 0; x < DPL; ++x) {
+        const int d = DPL * lane + x;
+        o[x] += pt * (cached(c.v, (tt & ~(size_t)15) * HD + (size_t)d * GRAN + (tt & 15)) * vsc);
+      }
+    }
+  }
+  const bool any = l != 0.f;
+  if (a.part) {
+    float* x = a.part + ((r * a.hq + h) * a.nsplit_ld + split) * (HD + 2);
+#pragma unroll
+    for (int e = 0; e < DPL; ++e) x[DPL * lane + e] = o[e];
+    if (lane == 0) {
+      x[HD] = m * LN2;
+      x[HD + 1] = l;
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < DPL; ++e) {
+    const size_t at = r * a.ldo + (size_t)h * HD + DPL * lane + e;
+    const float y = any ? o[e] / l : 0.f;
+    if (QP == 1) ((bf16_t*)a.out)[at] = f2bf(y);
+    else ((float*)a.out)[at] = y;
+  }
+  if (lane == 0 && a.lse) a.lse[r * a.hq + h] = any ? m * LN2 + logf(l) : -INFINITY;
+}
+
+// Many rows: a workgroup of four waves owns 128 CBW query columns of one kv head of one
+// sequence (a wave 32 CBW of them) and walks the 64-key tiles of its split.  Wave w
+// brings granule w of a tile (16 keys, 16 values): loaded one tile ahead, widened to
+// bf16 once for all waves and put in LDS, where tiles alternate between two buffers,
+// one barrier a tile.  Products are 32x32x16: S^T = K Q^T, key row i of a 32-key block
+// being key 16 (i / 16) + 8 ((i / 4) % 2) + 4 ((i / 8) % 2) + i % 4, so that a lane's
+// scores are, in order, the probabilities of 8 consecutive tokens that O^T = V^T P^T
+// takes from it.
+//  keys in LDS    row r: its 16-byte chunk c at slot c ^ f(r) (f: the bits of r in
+//                 which the 8 lanes of a read differ)
+//  values in LDS  [granule][half of 8 tokens][dim], 16 bytes
+// Masked places as in k_pg_dec; where an infinite or NaN value lies between the
+// shortest and the longest length of a wave's columns they are computed again, one at
+// a time (`column`).
+template <int HD, bool E4, int QP, int CBW>
+__global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
+#pragma clang fp contract(off)
+  constexpr int PP = QP == 3 ? 3 : 1;
+  constexpr int NK = HD / 16;                 // contraction steps of a score
+  constexpr int ND = HD / 32;                 // blocks of 32 output dims
+  constexpr int LU = E4 ? HD / 64 : HD / 32;  // 16-byte loads a lane of a granule
+  constexpr int RB = 2 * HD;                  // bytes of a key row in LDS
+  __shared__ __align__(16) unsigned char s_k[2][KT * RB];
+  __shared__ __align__(16) unsigned char s_v[2][KT * RB];
+  __shared__ __align__(16) int s_ok[2][4], s_odd[2][4];
+  const PagedCache& c = a.cache;
+  const int G = a.hq / c.hkv;
+  const int lane = threadIdx.x & 63;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i32 = lane & 31, hf = lane >> 5;
+
+  int id = blockIdx.x;
+  const int kvh = id % c.hkv;
+  id /= c.hkv;
+  // blocks of late columns, which attend the most, first
+  const int col0 = (a.cblocks - 1 - id % a.cblocks) * 128 * CBW;
+  id /= a.cblocks;
+  const int b = id % a.rows.B, split = id / a.rows.B;
+  const int start = split * a.span;
+  const SeqRows sr = seq_rows(a.rows, b);
+  if (a.rows.err && threadIdx.x == 0 && sr.over) a.rows.err[b] = 1;
+  const int ncols = sr.n * G;
+  if (ncols <= col0 || ncols <= a.col_min) return;
+
+  // lengths: of this lane's columns, of the wave's, of the workgroup's
+  bool over = false;
+  int len[CBW], lmin = INT32_MAX, lmax = 0, wmax = 0;
+  const int wcol = col0 + 32 * CBW * w;  // the wave's first column
+#pragma unroll
+  for (int cb = 0; cb < CBW; ++cb) {
+    const int cc = min(wcol + 32 * cb + i32, ncols - 1);
+    len[cb] = row_len(a, sr, b, cc / G, over);
+    lmin = min(lmin, len[cb]);
+    lmax = max(lmax, len[cb]);
+  }
+  for (int cc = col0 + lane; cc < min(col0 + 128 * CBW, ncols); cc += 64)
+    wmax = max(wmax, row_len(a, sr, b, cc / G, over));
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    lmin = min(lmin, __shfl_xor(lmin, o));
+    lmax = max(lmax, __shfl_xor(lmax, o));
+    wmax = max(wmax, __shfl_xor(wmax, o));
+  }
+  lmin = __builtin_amdgcn_readfirstlane(lmin);
+  lmax = __builtin_amdgcn_readfirstlane(lmax);
+  wmax = __builtin_amdgcn_readfirstlane(wmax);
+  if (a.rows.err && __any(over)) a.rows.err[b] = 1;
+  const int stop = min(wmax, start + a.span);
+  if (start >= stop && split > 0) return;
+
+  // query columns
+  bf16x8 q[CBW][NK][QP];
+  constexpr size_t es = QP == 1 ? 2 : 4;
+#pragma unroll
+  for (int cb = 0; cb < CBW; ++cb) {
+    const int cc = min(wcol + 32 * cb + i32, ncols - 1);
+    const char* p = (const char*)a.q +
+                    ((size_t)(sr.r0 + cc / G) * a.ldq + (size_t)(kvh * G + cc % G) * HD) * es;
+#pragma unroll
+    for (int s = 0; s < NK; ++s) load_q<QP>(p + (16 * s + 8 * hf) * es, QP != 1, q[cb][s]);
+  }
+  f32x16 o[CBW][ND];
+  float m[CBW], l[CBW];
+#pragma unroll
+  for (int cb = 0; cb < CBW; ++cb) {
+    m[cb] = -FLT_MAX;
+    l[cb] = 0.f;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) o[cb][d][v] = 0.f;
+  }
+
+  // this wave's granule of a tile
+  const int* tab = a.rows.table + (size_t)b * a.rows.table_ld;
+  const int last_page = (a.rows.max_len - 1) >> c.lpage;
+  u32x4 kr[LU], vr[LU];
+  float ks = 1.f, vs = 1.f;
+  int pid = 0, pid_next = 0;  // its page, and the next tile's
+  auto ask = [&](int t0) { return tab[min((t0 + GRAN * w) >> c.lpage, last_page)]; };
+  bool ok = false;  // the registers' granule holds tokens
+  auto load = [&](int t0) {
+    const int p = t0 + GRAN * w;
+    pid = __builtin_amdgcn_readfirstlane(pid_next);
+    pid_next = ask(t0 + KT);
+    const bool in = pid >= 0 && pid < c.n_pages;
+    if (p < stop && !in && a.rows.err) a.rows.err[b] = 1;
+    ok = p < stop && in;
+    const size_t tok =
+        ok ? (((size_t)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1)) : 0;
+    const char* kp = (const char*)c.k + tok * HD * (E4 ? 1 : 2) + 16 * lane;
+    const char* vp = (const char*)c.v + tok * HD * (E4 ? 1 : 2) + 16 * lane;
+#pragma unroll
+    for (int u = 0; u < LU; ++u) kr[u] = *(const u32x4*)(kp + 1024 * u);
+#pragma unroll
+    for (int u = 0; u < LU; ++u) vr[u] = *(const u32x4*)(vp + 1024 * u);
+    if (E4) {
+      ks = c.k_scale[tok >> c.lblock];
+      vs = ok ? c.v_scale[tok >> c.lblock] : 1.f;
+    }
+  };
+  auto key_at = [](int r, int ch) {
+    return r * RB + ((ch ^ ((r & 3) | ((r >> 3) & 1) << 2)) << 4);
+  };
+  auto put = [&](int buf, int t0) {
+    const int n = ok ? min(stop - (t0 + GRAN * w), GRAN) : 0;  // its tokens
+    uint32_t odd = 0;
+#pragma unroll
+    for (int u = 0; u < LU; ++u) {
+      const int at = 1024 * u + 16 * lane;  // byte in the granule
+      if (E4) {
+        const int r = GRAN * w + at / HD, ch = at % HD / 8;
+        *(bf16x8*)(s_k[buf] + key_at(r, ch)) = widen(kr[u][0], kr[u][1], ks);
+        *(bf16x8*)(s_k[buf] + key_at(r, ch + 1)) = widen(kr[u][2], kr[u][3], ks);
+        u32x4 x = vr[u];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          x[y] &= bytes_below(n - 4 * y);
+          odd |= ((x[y] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+        }
+        unsigned char* p = s_v[buf] + (2 * w * HD + at / 16) * 16;
+        *(bf16x8*)p = widen(x[0], x[1], vs);
+        *(bf16x8*)(p + 16 * HD) = widen(x[2], x[3], vs);
+      } else {
+        *(u32x4*)(s_k[buf] + key_at(GRAN * w + at / RB, at % RB / 16)) = kr[u];
+        const int half = (at >> 4) & 1;
+        u32x4 x = vr[u];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          x[y] &= bytes_below(2 * (n - 8 * half - 2 * y));
+          const uint32_t z = x[y] & 0x7FFF7FFFu;
+          odd |= (z & 0xFFFFu) >= 0x7F80u || (z >> 16) >= 0x7F80u;
+        }
+        *(u32x4*)(s_v[buf] + ((2 * w + half) * HD + at / 32) * 16) = x;
+      }
+    }
+    const bool any = __any(odd != 0);
+    if (lane == 0) {
+      s_ok[buf][w] = ok;
+      s_odd[buf][w] = any;
+    }
+  };
+
+  const float sc = a.scale * LOG2E;
+  bool redo = false;
+  auto tile = [&](int buf, int t0, bool mask) {
+#pragma clang fp contract(off)
+    f32x16 s[CBW][2];
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb) {
+#pragma unroll
+      for (int cb = 0; cb < CBW; ++cb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[cb][kb][v] = 0.f;
+      const int r = 32 * kb + 16 * (i32 >> 4) + 8 * ((i32 >> 2) & 1) + 4 * ((i32 >> 3) & 1) + (i32 & 3);
+#pragma unroll
+      for (int st = 0; st < NK; ++st) {
+        const bf16x8 kk = *(const bf16x8*)(s_k[buf] + key_at(r, 2 * st + hf));
+#pragma unroll
+        for (int cb = 0; cb < CBW; ++cb)
+#pragma unroll
+          for (int n = 0; n < QP; ++n)
+            s[cb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[cb][st][n], s[cb][kb], 0, 0, 0);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // register v of block kb is token 32 kb + 16 (v / 8) + 8 hf + v % 8
+    bf16x8 p[CBW][4][PP];
+#pragma unroll
+    for (int cb = 0; cb < CBW; ++cb) {
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) s[cb][kb][v] *= sc;
+      if (mask) {
+        const int n = len[cb] - t0 - 8 * hf;
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const int gr = 2 * kb + (v >> 3);
+            if (!s_ok[buf][gr] || GRAN * gr + (v & 7) >= n) s[cb][kb][v] = -INFINITY;
+          }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[cb][kb][v]);
+      const float mn = fmaxf(m[cb], max_halves(mx));
+      if (__any(mn != m[cb])) {
+        const float al = __builtin_amdgcn_exp2f(m[cb] - mn);
+        m[cb] = mn;
+        l[cb] *= al;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) o[cb][d] *= al;
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const float e = __builtin_amdgcn_exp2f(s[cb][kb][v] - mn);
+          sum += e;
+          __bf16 y[PP];
+          planes_of<PP>(e, y);  // see k_pg_dec
+#pragma unroll
+          for (int n = 0; n < PP; ++n) p[cb][2 * kb + (v >> 3)][n][v & 7] = y[n];
+        }
+      l[cb] += sum;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int d = 0; d < ND; ++d) {
+#pragma unroll
+      for (int st = 0; st < 4; ++st) {
+        const bf16x8 vv = *(const bf16x8*)(s_v[buf] + ((2 * st + hf) * HD + 32 * d + i32) * 16);
+#pragma unroll
+        for (int cb = 0; cb < CBW; ++cb)
+#pragma unroll
+          for (int n = 0; n < PP; ++n)
+            o[cb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, p[cb][st][n], o[cb][d], 0, 0, 0);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+
+  if (start < stop) {
+    pid_next = ask(start);
+    load(start);
+    put(0, start);
+    load(start + KT);
+    __syncthreads();
+    int buf = 0;
+    for (int t0 = start; t0 < stop; t0 += KT, buf ^= 1) {
+      put(buf ^ 1, t0 + KT);
+      load(t0 + 2 * KT);
+      if (t0 < lmax) {
+        const int4 oks = *(const int4*)s_ok[buf], odds = *(const int4*)s_odd[buf];
+        const bool mask = !__all(t0 + KT <= lmin && oks.x && oks.y && oks.z && oks.w);
+        redo |= mask && __any(odds.x | odds.y | odds.z | odds.w);
+        tile(buf, t0, mask);
+      }
+      __syncthreads();
+    }
+  }
+  if (redo) {  // an infinite or NaN value where some columns must not see it
+    for (int cc = wcol; cc < min(wcol + 32 * CBW, ncols); ++cc)
+      column<HD, E4, QP>(a, sr, b, kvh, cc, start, stop, split);
+    return;
+  }
+
+  // results: lane (i32, hf) has dims 32 d + 8 (v / 4) + 4 hf + v % 4 of its column
+#pragma unroll
+  for (int cb = 0; cb < CBW; ++cb) {
+    l[cb] += __shfl_xor(l[cb], 32);
+    const int cc = wcol + 32 * cb + i32;
+    if (cc >= ncols || (a.part && len[cb] <= start)) continue;
+    const size_t r = sr.r0 + cc / G;
+    const int h = kvh * G + cc % G;
+    const bool any = l[cb] != 0.f;
+    const float inv = 1.0f / l[cb];
+    float* part = a.part ? a.part + ((r * a.hq + h) * a.nsplit_ld + split) * (HD + 2) : nullptr;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4) {
+        const int dim = 32 * d + 2 * v + 4 * hf;
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = o[cb][d][v + e];
+        if (part) {
+          *(float2*)(part + dim) = make_float2(y[0], y[1]);
+          *(float2*)(part + dim + 2) = make_float2(y[2], y[3]);
+          continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = any ? y[e] * inv : 0.f;
+        const size_t at = r * a.ldo + (size_t)h * HD + dim;
+        if (QP == 1) {
+          bf16_t z[4] = {f2bf(y[0]), f2bf(y[1]), f2bf(y[2]), f2bf(y[3])};
+          *(uint2*)((bf16_t*)a.out + at) = *(const uint2*)z;
+        } else {
+          *(float4*)((float*)a.out + at) = make_float4(y[0], y[1], y[2], y[3]);
+        }
+      }
+    if (hf == 0) {
+      if (part) *(float2*)(part + HD) = make_float2(m[cb] * LN2, l[cb]);
+      else if (a.lse) a.lse[r * a.hq + h] = any ? m[cb] * LN2 + logf(l[cb]) : -INFINITY;
+    }
+  }
+}
+
 // NW waves per (row, query head) join the splits that hold keys of the row, each of
 // them every NW-th, in order, then the waves' results.  Partials are (o[hd], max,
 // sum) with the maximum in natural units.  The first partials are requested before
@@ -834,7 +1229,7 @@ __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
   bool mine = job < a.rows.rows * a.hq && b >= 0;
   if (mine) {
     const SeqRows sr = seq_rows(a.rows, b);
-    mine = r - sr.r0 < sr.n && sr.n * (a.hq / a.cache.hkv) <= a.col_max;
+    mine = r - sr.r0 < sr.n;
     bool over = false;
     ns = (row_len(a, sr, b, r - sr.r0, over) + a.span - 1) / a.span;
   }
@@ -909,48 +1304,81 @@ void paged_append(const PagedAppend& a, hipStream_t st) {
 #undef KS_APP
 }
 
-// Splits: as many as give every CU a workgroup (one sequence of 32768 tokens: 17.8 us
-// with 256 workgroups, 21.1 with 384 and 27.5 with 1024, the rest being their start
-// and the merge), none shorter than a tile for every wave, and none longer than 4096
-// positions, which keeps sequences of different lengths level (64 of 500 to 15000
-// tokens: 216 us, 225 to 250 with one split each).
-int paged_splits(int B, int hkv, int G, int max_rows, int max_len) {
-  const int blocks = B * hkv * ((max_rows * G + 31) / 32);
-  const int most = std::max(1, (max_len + DEC_NW * KT - 1) / (DEC_NW * KT));
-  return std::min(std::max((255 + blocks) / blocks, (max_len + 4095) / 4096), most);
+// Which kernel: a sequence of up to DEC_COLS query columns (rows times query heads of
+// a kv head) goes to the split kernel, one of more to the chunk kernel.
+constexpr int DEC_COLS = 64;
+
+PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int planes) {
+  PagedPlan p{};
+  const int cols = max_rows * G;
+  const bool chunk = cols > DEC_COLS;
+  // Splits of the split kernel: as many as give every CU a workgroup (one sequence of
+  // 32768 tokens: 17.8 us with 256 workgroups, 21.1 with 384 and 27.5 with 1024, the
+  // rest being their start and the merge), none shorter than a tile for every wave,
+  // and none longer than 4096 positions, which keeps sequences of different lengths
+  // level (64 of 500 to 15000 tokens: 216 us, 225 to 250 with one split each).
+  // Of the chunk kernel: what fills the CUs, none shorter than 8 tiles.
+  const int width = chunk ? (planes == 1 ? 256 : 128) : 32;
+  const int blocks = B * hkv * ((cols + width - 1) / width);
+  const int least = chunk ? 8 * KT : DEC_NW * KT;
+  const int most = std::max(1, (max_len + least - 1) / least);
+  int want = chunk ? 256 / std::max(1, std::min(blocks, 256)) : (255 + blocks) / blocks;
+  if (!chunk || B > 1) want = std::max(want, (max_len + 4095) / 4096);
+  p.chunk = chunk;
+  p.nsplit = std::max(1, std::min(want, most));
+  p.span = ((max_len + p.nsplit - 1) / p.nsplit + KT - 1) / KT * KT;
+  return p;
 }
 
 void paged_attention(const PagedAttn& a_, hipStream_t st) {
   PagedAttn a = a_;
   const PagedCache& c = a.cache;
   const int G = a.hq / c.hkv;
-  a.col_max = INT32_MAX;
-  const int cols = a.rows.max_rows * G;
-  const int CB = cols <= 16 ? 1 : 2;
-  a.cblocks = (cols + 16 * CB - 1) / (16 * CB);
-  const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
-  a.lds_pages = (a.span / c.page + 2) * 4 + 15 & ~15;
   const int planes = a.planes ? a.planes : a.dtype == KS_BF16 ? 1 : 3;
-  const size_t lds = std::max((size_t)DEC_NW * 16 * CB * (c.hd + 4) * 4,
-                              (size_t)a.lds_pages + CB * c.hd / 32 * planes * 1024 +
-                                  DEC_NW * KT * c.hd * (c.kind == KS_E4M3 ? 1 : 2));
+  const bool chunk = !a.few && a.rows.max_rows * G > DEC_COLS;
+#define KS_ATT_T(X_, QP_)                                              \
+  do {                                                                 \
+    if (c.hd == 128 && c.kind == KS_E4M3) X_(128, true, QP_);          \
+    else if (c.hd == 128) X_(128, false, QP_);                         \
+    else if (c.kind == KS_E4M3) X_(64, true, QP_);                     \
+    else X_(64, false, QP_);                                           \
+  } while (0)
+#define KS_ATT(X_)                                                     \
+  do {                                                                 \
+    if (planes == 1) KS_ATT_T(X_, 1);                                  \
+    else if (planes == 2) KS_ATT_T(X_, 2);                             \
+    else KS_ATT_T(X_, 3);                                              \
+  } while (0)
+  if (chunk) {
+    const int width = planes == 1 ? 256 : 128;
+    a.col_min = a.rows.B > 1 ? DEC_COLS : 0;  // shorter sequences: below
+    a.cblocks = (a.rows.max_rows * G + width - 1) / width;
+    const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
+#define KS_CHK(HD_, E_, QP_) \
+  KS_LAUNCH((k_pg_chunk<HD_, E_, QP_, QP_ == 1 ? 2 : 1>), grid, dim3(256), 0, st, a)
+    KS_ATT(KS_CHK);
+#undef KS_CHK
+  }
+  if (!chunk || a.rows.B > 1) {
+    a.col_max = chunk ? DEC_COLS : INT32_MAX;
+    const int cols = std::min(a.rows.max_rows * G, a.col_max);
+    const int CB = cols <= 16 ? 1 : 2;
+    a.cblocks = (cols + 16 * CB - 1) / (16 * CB);
+    const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
+    a.lds_pages = (a.span / c.page + 2) * 4 + 15 & ~15;
+    const size_t lds = std::max((size_t)DEC_NW * 16 * CB * (c.hd + 4) * 4,
+                                (size_t)a.lds_pages + CB * c.hd / 32 * planes * 1024 +
+                                    DEC_NW * KT * c.hd * (c.kind == KS_E4M3 ? 1 : 2));
 #define KS_DEC(HD_, E_, QP_)                                                              \
   do {                                                                                    \
     if (CB == 1) KS_LAUNCH((k_pg_dec<HD_, E_, QP_, 1>), grid, dim3(256), lds, st, a);     \
     else KS_LAUNCH((k_pg_dec<HD_, E_, QP_, 2>), grid, dim3(256), lds, st, a);             \
   } while (0)
-#define KS_DEC_T(QP_)                                                  \
-  do {                                                                 \
-    if (c.hd == 128 && c.kind == KS_E4M3) KS_DEC(128, true, QP_);      \
-    else if (c.hd == 128) KS_DEC(128, false, QP_);                     \
-    else if (c.kind == KS_E4M3) KS_DEC(64, true, QP_);                 \
-    else KS_DEC(64, false, QP_);                                       \
-  } while (0)
-  if (planes == 1) KS_DEC_T(1);
-  else if (planes == 2) KS_DEC_T(2);
-  else KS_DEC_T(3);
-#undef KS_DEC_T
+    KS_ATT(KS_DEC);
 #undef KS_DEC
+  }
+#undef KS_ATT
+#undef KS_ATT_T
   if (!a.part || !a.out) return;
   // up to eight splits are one wave's loads
   const int per = a.nsplit > 8 ? 1 : 4;  // (row, head) pairs of a workgroup

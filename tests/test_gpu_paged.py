@@ -305,6 +305,23 @@ def test_rollback_and_padding(E, kind):
     x.step([2, 3, 4])
 
 
+@pytest.mark.parametrize("c", [
+    (3, 8, 2, 128, 64, 16, "e4m3", "bf16", 7), (2, 4, 2, 128, 16, 16, "bf16", "bf16", 25),
+    (2, 6, 2, 64, 32, 32, "e4m3", "f32", 14), (1, 3, 1, 128, 128, 64, "e4m3", "f32", 3),
+    (2, 5, 1, 64, 16, 16, "bf16", "bf16", 25), (2, 2, 2, 128, 256, 32, "bf16", "f32", 2)],
+    ids=lambda c: "-".join(map(str, c)))
+def test_chunks(E, c):
+    """Prompt chunks next to single tokens and an empty sequence, then a chunk that
+    continues its own prompt."""
+    print("chunks", c, flush=True)
+    B = c[0]
+    x = Case(E, *c, seed=20 + B)
+    cap = c[8] * c[4]
+    x.step([(151, 1, 0)[b] for b in range(B)])
+    x.step([(cap - 155, 70, 3)[b] for b in range(B)], std=0.7)
+    x.step([(1, 90, 129)[b] for b in range(B)], tail=2)
+
+
 def test_same_rows_again_and_no_queries(E):
     x = Case(E, *SMALL, seed=6)
     x.step([9, 21, 40])
