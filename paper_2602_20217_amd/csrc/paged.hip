@@ -554,7 +554,8 @@ __global__ __launch_bounds__(64 * DEC_NW, dec_wgs(HD, E4, QP, CB)) void k_pg_dec
   // One tile whose keys lie in LDS and whose values are in flight.  MASK: some of its
   // keys are past a column's length or on an invalid page.  Both forms compute the
   // same bits of what is not masked.
-  auto tile = [&](auto mask_, int t0, bool have, float ksc, float vsc) {
+  auto tile = [&](auto mask_, int t0, bool have, float ksc,
+                  float vsc) __attribute__((always_inline)) {
 #pragma clang fp contract(off)
     constexpr bool MASK = decltype(mask_)::value;
     // scores: row 4 g + v of subtile kt is key 16 g + 4 kt + v, column lane % 16
@@ -815,7 +816,7 @@ __device__ inline float max_halves(float x) {
 // One column by a wave, without matrix instructions: lanes take keys, then dims.  Only
 // what it attends is read.
 template <int HD, bool E4, int QP>
-__device__ __attribute__((noinline)) void column(const PagedAttn& a, const SeqRows& sr, int b,
+__device__ inline void column(const PagedAttn& a, const SeqRows& sr, int b,
                                                  int kvh, int cc, int start, int stop, int split) {
   constexpr int DPL = HD / 64;
   const PagedCache& c = a.cache;
@@ -884,22 +885,23 @@ __device__ __attribute__((noinline)) void column(const PagedAttn& a, const SeqRo
   if (lane == 0 && a.lse) a.lse[r * a.hq + h] = any ? m * LN2 + logf(l) : -INFINITY;
 }
 
-// Many rows: a workgroup of four waves owns 128 CBW query columns of one kv head of one
-// sequence (a wave 32 CBW of them) and walks the 64-key tiles of its split.  Wave w
+// Many rows: a workgroup of four waves owns 128 query columns of one kv head of one
+// sequence (a wave 32 of them) and walks the 64-key tiles of its split.  Wave w
 // brings granule w of a tile (16 keys, 16 values): loaded one tile ahead, widened to
 // bf16 once for all waves and put in LDS, where tiles alternate between two buffers,
 // one barrier a tile.  Products are 32x32x16: S^T = K Q^T, key row i of a 32-key block
 // being key 16 (i / 16) + 8 ((i / 4) % 2) + 4 ((i / 8) % 2) + i % 4, so that a lane's
 // scores are, in order, the probabilities of 8 consecutive tokens that O^T = V^T P^T
 // takes from it.
-//  keys in LDS    row r: its 16-byte chunk c at slot c ^ f(r) (f: the bits of r in
-//                 which the 8 lanes of a read differ)
+//  keys in LDS    row r: its 16-byte chunk c at slot c ^ f(r) ^ c / 8 (f: the bits of
+//                 r in which the 8 lanes of a read differ; those of a write have
+//                 every second chunk)
 //  values in LDS  [granule][half of 8 tokens][dim], 16 bytes
 // Masked places as in k_pg_dec; where an infinite or NaN value lies between the
 // shortest and the longest length of a wave's columns they are computed again, one at
 // a time (`column`).
-template <int HD, bool E4, int QP, int CBW>
-__global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
+template <int HD, bool E4, int QP>
+__global__ __launch_bounds__(256, 2) void k_pg_chunk(PagedAttn a) {
 #pragma clang fp contract(off)
   constexpr int PP = QP == 3 ? 3 : 1;
   constexpr int NK = HD / 16;                 // contraction steps of a score
@@ -919,7 +921,7 @@ __global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
   const int kvh = id % c.hkv;
   id /= c.hkv;
   // blocks of late columns, which attend the most, first
-  const int col0 = (a.cblocks - 1 - id % a.cblocks) * 128 * CBW;
+  const int col0 = (a.cblocks - 1 - id % a.cblocks) * 128;
   id /= a.cblocks;
   const int b = id % a.rows.B, split = id / a.rows.B;
   const int start = split * a.span;
@@ -930,23 +932,23 @@ __global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
 
   // lengths: of this lane's columns, of the wave's, of the workgroup's
   bool over = false;
-  int len[CBW], lmin = INT32_MAX, lmax = 0, wmax = 0;
-  const int wcol = col0 + 32 * CBW * w;  // the wave's first column
-#pragma unroll
-  for (int cb = 0; cb < CBW; ++cb) {
-    const int cc = min(wcol + 32 * cb + i32, ncols - 1);
-    len[cb] = row_len(a, sr, b, cc / G, over);
-    lmin = min(lmin, len[cb]);
-    lmax = max(lmax, len[cb]);
+  const int wcol = col0 + 32 * w;  // the wave's first column
+  const int col = min(wcol + i32, ncols - 1);
+  const int len = row_len(a, sr, b, col / G, over);
+  int lmin = len, lmax = len, wmin = INT32_MAX, wmax = 0;
+  for (int x = 0; x < 2; ++x) {
+    const int n = row_len(a, sr, b, min(col0 + 64 * x + lane, ncols - 1) / G, over);
+    wmin = min(wmin, n);
+    wmax = max(wmax, n);
   }
-  for (int cc = col0 + lane; cc < min(col0 + 128 * CBW, ncols); cc += 64)
-    wmax = max(wmax, row_len(a, sr, b, cc / G, over));
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) {
     lmin = min(lmin, __shfl_xor(lmin, o));
     lmax = max(lmax, __shfl_xor(lmax, o));
+    wmin = min(wmin, __shfl_xor(wmin, o));
     wmax = max(wmax, __shfl_xor(wmax, o));
   }
+  wmin = __builtin_amdgcn_readfirstlane(wmin);
   lmin = __builtin_amdgcn_readfirstlane(lmin);
   lmax = __builtin_amdgcn_readfirstlane(lmax);
   wmax = __builtin_amdgcn_readfirstlane(wmax);
@@ -955,45 +957,42 @@ __global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
   if (start >= stop && split > 0) return;
 
   // query columns
-  bf16x8 q[CBW][NK][QP];
+  bf16x8 q[NK][QP];
   constexpr size_t es = QP == 1 ? 2 : 4;
+  const char* qp = (const char*)a.q +
+                   ((size_t)(sr.r0 + col / G) * a.ldq + (size_t)(kvh * G + col % G) * HD) * es;
 #pragma unroll
-  for (int cb = 0; cb < CBW; ++cb) {
-    const int cc = min(wcol + 32 * cb + i32, ncols - 1);
-    const char* p = (const char*)a.q +
-                    ((size_t)(sr.r0 + cc / G) * a.ldq + (size_t)(kvh * G + cc % G) * HD) * es;
+  for (int s = 0; s < NK; ++s) {
+    load_q<QP>(qp + (16 * s + 8 * hf) * es, QP != 1, q[s]);
+    if (a.scale < 0.f)
 #pragma unroll
-    for (int s = 0; s < NK; ++s) load_q<QP>(p + (16 * s + 8 * hf) * es, QP != 1, q[cb][s]);
+      for (int n = 0; n < QP; ++n)
+        q[s][n] = __builtin_bit_cast(bf16x8, __builtin_bit_cast(u32x4, q[s][n]) ^ 0x80008000u);
   }
-  f32x16 o[CBW][ND];
-  float m[CBW], l[CBW];
+  f32x16 o[ND];
+  float m = -FLT_MAX, l = 0.f;
 #pragma unroll
-  for (int cb = 0; cb < CBW; ++cb) {
-    m[cb] = -FLT_MAX;
-    l[cb] = 0.f;
+  for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) o[cb][d][v] = 0.f;
-  }
+    for (int v = 0; v < 16; ++v) o[d][v] = 0.f;
 
   // this wave's granule of a tile
   const int* tab = a.rows.table + (size_t)b * a.rows.table_ld;
   const int last_page = (a.rows.max_len - 1) >> c.lpage;
   u32x4 kr[LU], vr[LU];
   float ks = 1.f, vs = 1.f;
-  int pid = 0, pid_next = 0;  // its page, and the next tile's
+  int pid_next = 0;  // the next tile's page
   auto ask = [&](int t0) { return tab[min((t0 + GRAN * w) >> c.lpage, last_page)]; };
-  bool ok = false;  // the registers' granule holds tokens
-  auto load = [&](int t0) {
+  int n_tok = 0;  // tokens of the registers' granule
+  auto load = [&](int t0) __attribute__((always_inline)) {
     const int p = t0 + GRAN * w;
-    pid = __builtin_amdgcn_readfirstlane(pid_next);
+    const int pid = __builtin_amdgcn_readfirstlane(pid_next);
     pid_next = ask(t0 + KT);
     const bool in = pid >= 0 && pid < c.n_pages;
     if (p < stop && !in && a.rows.err) a.rows.err[b] = 1;
-    ok = p < stop && in;
+    n_tok = in ? min(max(stop - p, 0), GRAN) : 0;
     const size_t tok =
-        ok ? (((size_t)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1)) : 0;
+        n_tok > 0 ? (((size_t)pid * c.hkv + kvh) << c.lpage) + (p & (c.page - 1)) : 0;
     const char* kp = (const char*)c.k + tok * HD * (E4 ? 1 : 2) + 16 * lane;
     const char* vp = (const char*)c.v + tok * HD * (E4 ? 1 : 2) + 16 * lane;
 #pragma unroll
@@ -1002,15 +1001,33 @@ __global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
     for (int u = 0; u < LU; ++u) vr[u] = *(const u32x4*)(vp + 1024 * u);
     if (E4) {
       ks = c.k_scale[tok >> c.lblock];
-      vs = ok ? c.v_scale[tok >> c.lblock] : 1.f;
+      vs = c.v_scale[tok >> c.lblock];
     }
   };
   auto key_at = [](int r, int ch) {
-    return r * RB + ((ch ^ ((r & 3) | ((r >> 3) & 1) << 2)) << 4);
+    return r * RB + ((ch ^ ((r & 3) | ((r >> 3) & 1) << 2) ^ (ch >> 3)) << 4);
   };
-  auto put = [&](int buf, int t0) {
-    const int n = ok ? min(stop - (t0 + GRAN * w), GRAN) : 0;  // its tokens
-    uint32_t odd = 0;
+  // into buffer buf; ragged: some column does not attend all of the tile
+  auto put = [&](int buf, bool ragged) __attribute__((always_inline)) {
+    if (ragged || n_tok < GRAN) {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int u = 0; u < LU; ++u)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          if (E4) {
+            vr[u][y] &= bytes_below(n_tok - 4 * y);
+            odd |= ((vr[u][y] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+          } else {
+            vr[u][y] &= bytes_below(2 * (n_tok - 8 * (lane & 1) - 2 * y));
+            const uint32_t z = vr[u][y] & 0x7FFF7FFFu;
+            odd |= (z & 0xFFFFu) >= 0x7F80u || (z >> 16) >= 0x7F80u;
+          }
+        }
+      const bool any = __any(odd != 0);
+      if (lane == 0) s_odd[buf][w] = any;
+      if (n_tok == 0) vs = 1.f;
+    }
 #pragma unroll
     for (int u = 0; u < LU; ++u) {
       const int at = 1024 * u + 16 * lane;  // byte in the granule
@@ -1018,182 +1035,153 @@ __global__ __launch_bounds__(256, 1) void k_pg_chunk(PagedAttn a) {
         const int r = GRAN * w + at / HD, ch = at % HD / 8;
         *(bf16x8*)(s_k[buf] + key_at(r, ch)) = widen(kr[u][0], kr[u][1], ks);
         *(bf16x8*)(s_k[buf] + key_at(r, ch + 1)) = widen(kr[u][2], kr[u][3], ks);
-        u32x4 x = vr[u];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          x[y] &= bytes_below(n - 4 * y);
-          odd |= ((x[y] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
-        }
         unsigned char* p = s_v[buf] + (2 * w * HD + at / 16) * 16;
-        *(bf16x8*)p = widen(x[0], x[1], vs);
-        *(bf16x8*)(p + 16 * HD) = widen(x[2], x[3], vs);
+        *(bf16x8*)p = widen(vr[u][0], vr[u][1], vs);
+        *(bf16x8*)(p + 16 * HD) = widen(vr[u][2], vr[u][3], vs);
       } else {
         *(u32x4*)(s_k[buf] + key_at(GRAN * w + at / RB, at % RB / 16)) = kr[u];
-        const int half = (at >> 4) & 1;
-        u32x4 x = vr[u];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          x[y] &= bytes_below(2 * (n - 8 * half - 2 * y));
-          const uint32_t z = x[y] & 0x7FFF7FFFu;
-          odd |= (z & 0xFFFFu) >= 0x7F80u || (z >> 16) >= 0x7F80u;
-        }
-        *(u32x4*)(s_v[buf] + ((2 * w + half) * HD + at / 32) * 16) = x;
+        *(u32x4*)(s_v[buf] + ((2 * w + (lane & 1)) * HD + at / 32) * 16) = vr[u];
       }
     }
-    const bool any = __any(odd != 0);
-    if (lane == 0) {
-      s_ok[buf][w] = ok;
-      s_odd[buf][w] = any;
-    }
+    if (lane == 0) s_ok[buf][w] = n_tok;
   };
 
-  const float sc = a.scale * LOG2E;
+  const float sc = fmaxf(fabsf(a.scale) * LOG2E, FLT_MIN);  // > 0: times -inf no NaN
   bool redo = false;
-  auto tile = [&](int buf, int t0, bool mask) {
+  auto tile = [&](int buf, int t0, bool mask) __attribute__((always_inline)) {
 #pragma clang fp contract(off)
-    f32x16 s[CBW][2];
+    f32x16 s[2];
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) {
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int cb = 0; cb < CBW; ++cb)
+      for (int v = 0; v < 16; ++v) s[kb][v] = 0.f;
+    const int r = 16 * (i32 >> 4) + 8 * ((i32 >> 2) & 1) + 4 * ((i32 >> 3) & 1) + (i32 & 3);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) s[cb][kb][v] = 0.f;
-      const int r = 32 * kb + 16 * (i32 >> 4) + 8 * ((i32 >> 2) & 1) + 4 * ((i32 >> 3) & 1) + (i32 & 3);
+    for (int st = 0; st < NK; ++st)
 #pragma unroll
-      for (int st = 0; st < NK; ++st) {
-        const bf16x8 kk = *(const bf16x8*)(s_k[buf] + key_at(r, 2 * st + hf));
+      for (int kb = 0; kb < 2; ++kb) {
+        const bf16x8 kk = *(const bf16x8*)(s_k[buf] + key_at(r + 32 * kb, 2 * st + hf));
 #pragma unroll
-        for (int cb = 0; cb < CBW; ++cb)
-#pragma unroll
-          for (int n = 0; n < QP; ++n)
-            s[cb][kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[cb][st][n], s[cb][kb], 0, 0, 0);
+        for (int n = 0; n < QP; ++n)
+          s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, q[st][n], s[kb], 0, 0, 0);
       }
-    }
-    __builtin_amdgcn_sched_barrier(0);
     // register v of block kb is token 32 kb + 16 (v / 8) + 8 hf + v % 8
-    bf16x8 p[CBW][4][PP];
-#pragma unroll
-    for (int cb = 0; cb < CBW; ++cb) {
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) s[cb][kb][v] *= sc;
-      if (mask) {
-        const int n = len[cb] - t0 - 8 * hf;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) {
-            const int gr = 2 * kb + (v >> 3);
-            if (!s_ok[buf][gr] || GRAN * gr + (v & 7) >= n) s[cb][kb][v] = -INFINITY;
-          }
-      }
-      float mx = -INFINITY;
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[cb][kb][v]);
-      const float mn = fmaxf(m[cb], max_halves(mx));
-      if (__any(mn != m[cb])) {
-        const float al = __builtin_amdgcn_exp2f(m[cb] - mn);
-        m[cb] = mn;
-        l[cb] *= al;
-#pragma unroll
-        for (int d = 0; d < ND; ++d) o[cb][d] *= al;
-      }
-      float sum = 0.f;
+    if (mask) {
+      const int n = len - t0 - 8 * hf;
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          const float e = __builtin_amdgcn_exp2f(s[cb][kb][v] - mn);
-          sum += e;
-          __bf16 y[PP];
-          planes_of<PP>(e, y);  // see k_pg_dec
-#pragma unroll
-          for (int n = 0; n < PP; ++n) p[cb][2 * kb + (v >> 3)][n][v & 7] = y[n];
+          const int gr = 2 * kb + (v >> 3);
+          if (!s_ok[buf][gr] || GRAN * gr + (v & 7) >= n) s[kb][v] = -INFINITY;
         }
-      l[cb] += sum;
-      __builtin_amdgcn_sched_barrier(0);
     }
+    float mx = -INFINITY;
 #pragma unroll
-    for (int d = 0; d < ND; ++d) {
+    for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-      for (int st = 0; st < 4; ++st) {
+      for (int v = 0; v < 16; ++v) mx = fmaxf(mx, s[kb][v]);
+    // queries carry the scale's sign, so sc > 0
+    const float mn = fmaxf(m, max_halves(mx) * sc);
+    if (__any(mn != m)) {
+      const float al = __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= al;
+#pragma unroll
+      for (int d = 0; d < ND; ++d) o[d] *= al;
+    }
+    bf16x8 p[4][PP];
+    float sum = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[kb][v], sc, -mn));
+        sum += e;
+        __bf16 y[PP];
+        planes_of<PP>(e, y);  // see k_pg_dec
+#pragma unroll
+        for (int n = 0; n < PP; ++n) p[2 * kb + (v >> 3)][n][v & 7] = y[n];
+      }
+    l += sum;
+#pragma unroll
+    for (int st = 0; st < 4; ++st)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
         const bf16x8 vv = *(const bf16x8*)(s_v[buf] + ((2 * st + hf) * HD + 32 * d + i32) * 16);
 #pragma unroll
-        for (int cb = 0; cb < CBW; ++cb)
-#pragma unroll
-          for (int n = 0; n < PP; ++n)
-            o[cb][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, p[cb][st][n], o[cb][d], 0, 0, 0);
+        for (int n = 0; n < PP; ++n)
+          o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vv, p[st][n], o[d], 0, 0, 0);
       }
-      __builtin_amdgcn_sched_barrier(0);
-    }
   };
 
+  // tile t0 lies in buffer buf, the next one in the registers
+  auto step = [&](auto buf_, int t0) __attribute__((always_inline)) {
+    constexpr int buf = decltype(buf_)::value;
+    put(buf ^ 1, t0 + 2 * KT > wmin);
+    load(t0 + 2 * KT);
+    if (t0 < lmax) {
+      const int4 ok = *(const int4*)s_ok[buf];
+      const bool mask = !__all(t0 + KT <= lmin && ok.x && ok.y && ok.z && ok.w);
+      if (mask && t0 + KT > wmin) {
+        const int4 odd = *(const int4*)s_odd[buf];
+        redo |= __any(odd.x | odd.y | odd.z | odd.w);
+      }
+      tile(buf, t0, mask);
+    }
+    __syncthreads();
+  };
   if (start < stop) {
     pid_next = ask(start);
     load(start);
-    put(0, start);
+    put(0, start + KT > wmin);
     load(start + KT);
     __syncthreads();
-    int buf = 0;
-    for (int t0 = start; t0 < stop; t0 += KT, buf ^= 1) {
-      put(buf ^ 1, t0 + KT);
-      load(t0 + 2 * KT);
-      if (t0 < lmax) {
-        const int4 oks = *(const int4*)s_ok[buf], odds = *(const int4*)s_odd[buf];
-        const bool mask = !__all(t0 + KT <= lmin && oks.x && oks.y && oks.z && oks.w);
-        redo |= mask && __any(odds.x | odds.y | odds.z | odds.w);
-        tile(buf, t0, mask);
-      }
-      __syncthreads();
+    for (int t0 = start; t0 < stop; t0 += 2 * KT) {
+      step(std::integral_constant<int, 0>{}, t0);
+      if (t0 + KT < stop) step(std::integral_constant<int, 1>{}, t0 + KT);
     }
   }
   if (redo) {  // an infinite or NaN value where some columns must not see it
-    for (int cc = wcol; cc < min(wcol + 32 * CBW, ncols); ++cc)
+    for (int cc = wcol; cc < min(wcol + 32, ncols); ++cc)
       column<HD, E4, QP>(a, sr, b, kvh, cc, start, stop, split);
     return;
   }
 
   // results: lane (i32, hf) has dims 32 d + 8 (v / 4) + 4 hf + v % 4 of its column
+  l += __shfl_xor(l, 32);
+  if (wcol + i32 >= ncols || (a.part && len <= start)) return;
+  const size_t r = sr.r0 + col / G;
+  const int h = kvh * G + col % G;
+  const bool any = l != 0.f;
+  const float inv = 1.0f / l;
+  float* part = a.part ? a.part + ((r * a.hq + h) * a.nsplit_ld + split) * (HD + 2) : nullptr;
 #pragma unroll
-  for (int cb = 0; cb < CBW; ++cb) {
-    l[cb] += __shfl_xor(l[cb], 32);
-    const int cc = wcol + 32 * cb + i32;
-    if (cc >= ncols || (a.part && len[cb] <= start)) continue;
-    const size_t r = sr.r0 + cc / G;
-    const int h = kvh * G + cc % G;
-    const bool any = l[cb] != 0.f;
-    const float inv = 1.0f / l[cb];
-    float* part = a.part ? a.part + ((r * a.hq + h) * a.nsplit_ld + split) * (HD + 2) : nullptr;
+  for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int d = 0; d < ND; ++d)
+    for (int v = 0; v < 16; v += 4) {
+      const int dim = 32 * d + 2 * v + 4 * hf;
+      float y[4];
 #pragma unroll
-      for (int v = 0; v < 16; v += 4) {
-        const int dim = 32 * d + 2 * v + 4 * hf;
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = o[cb][d][v + e];
-        if (part) {
-          *(float2*)(part + dim) = make_float2(y[0], y[1]);
-          *(float2*)(part + dim + 2) = make_float2(y[2], y[3]);
-          continue;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = any ? y[e] * inv : 0.f;
-        const size_t at = r * a.ldo + (size_t)h * HD + dim;
-        if (QP == 1) {
-          bf16_t z[4] = {f2bf(y[0]), f2bf(y[1]), f2bf(y[2]), f2bf(y[3])};
-          *(uint2*)((bf16_t*)a.out + at) = *(const uint2*)z;
-        } else {
-          *(float4*)((float*)a.out + at) = make_float4(y[0], y[1], y[2], y[3]);
-        }
+      for (int e = 0; e < 4; ++e) y[e] = o[d][v + e];
+      if (part) {
+        *(float2*)(part + dim) = make_float2(y[0], y[1]);
+        *(float2*)(part + dim + 2) = make_float2(y[2], y[3]);
+        continue;
       }
-    if (hf == 0) {
-      if (part) *(float2*)(part + HD) = make_float2(m[cb] * LN2, l[cb]);
-      else if (a.lse) a.lse[r * a.hq + h] = any ? m[cb] * LN2 + logf(l[cb]) : -INFINITY;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = any ? y[e] * inv : 0.f;
+      const size_t at = r * a.ldo + (size_t)h * HD + dim;
+      if (QP == 1) {
+        bf16_t z[4] = {f2bf(y[0]), f2bf(y[1]), f2bf(y[2]), f2bf(y[3])};
+        *(uint2*)((bf16_t*)a.out + at) = *(const uint2*)z;
+      } else {
+        *(float4*)((float*)a.out + at) = make_float4(y[0], y[1], y[2], y[3]);
+      }
     }
+  if (hf == 0) {
+    if (part) *(float2*)(part + HD) = make_float2(m * LN2, l);
+    else if (a.lse) a.lse[r * a.hq + h] = any ? m * LN2 + logf(l) : -INFINITY;
   }
 }
 
@@ -1318,7 +1306,7 @@ PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int plane
   // and none longer than 4096 positions, which keeps sequences of different lengths
   // level (64 of 500 to 15000 tokens: 216 us, 225 to 250 with one split each).
   // Of the chunk kernel: what fills the CUs, none shorter than 8 tiles.
-  const int width = chunk ? (planes == 1 ? 256 : 128) : 32;
+  const int width = chunk ? (128) : 32;
   const int blocks = B * hkv * ((cols + width - 1) / width);
   const int least = chunk ? 8 * KT : DEC_NW * KT;
   const int most = std::max(1, (max_len + least - 1) / least);
@@ -1350,12 +1338,12 @@ void paged_attention(const PagedAttn& a_, hipStream_t st) {
     else KS_ATT_T(X_, 3);                                              \
   } while (0)
   if (chunk) {
-    const int width = planes == 1 ? 256 : 128;
+    const int width = 128;
     a.col_min = a.rows.B > 1 ? DEC_COLS : 0;  // shorter sequences: below
     a.cblocks = (a.rows.max_rows * G + width - 1) / width;
     const dim3 grid((unsigned)((size_t)a.nsplit * c.hkv * a.cblocks * a.rows.B));
 #define KS_CHK(HD_, E_, QP_) \
-  KS_LAUNCH((k_pg_chunk<HD_, E_, QP_, QP_ == 1 ? 2 : 1>), grid, dim3(256), 0, st, a)
+  KS_LAUNCH((k_pg_chunk<HD_, E_, QP_>), grid, dim3(256), 0, st, a)
     KS_ATT(KS_CHK);
 #undef KS_CHK
   }
