@@ -252,6 +252,7 @@ struct PagedAppend {
   const float* k_gain = nullptr;
   float eps = 0.f;
   int perm = 0;
+  int vec = 0;  // set by paged_append: q, q_out, k, v rows at 16-byte addresses
 };
 void paged_append(const PagedAppend& a, hipStream_t st);
 // Row i of sequence b attends positions [0, pos0[b] + i], or [0, len[row]).

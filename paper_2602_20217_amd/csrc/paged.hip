@@ -119,59 +119,151 @@ __device__ inline int seq_of(const PagedRows& s, int r) {
 }
 
 // ------------------------------------------------------------------- append
-// Rotation of the pair (f, f + hd/2) of a head by the table's angle of its
-// position, after an optional RMS norm over the head (gain != nullptr).
-// LT = hd/2 lanes hold one row, lane f its pair.
-template <int LT>
-__device__ inline float2 turn(float x0, float x1, const float* cs, const float* gain, float eps,
-                              int f) {
-  if (gain) {
-    const float ss = group_sum<LT>(x0 * x0 + x1 * x1);
-    const float r = 1.0f / sqrtf(ss / (float)(2 * LT) + eps);
-    x0 = x0 * r * gain[f];
-    x1 = x1 * r * gain[f + LT];
+// 8 elements; vec: at a 16-byte address (wave-uniform)
+__device__ inline void load8(const float* p, bool vec, float (&x)[8]) {
+  if (vec) {
+    *(float4*)x = ((const float4*)p)[0];
+    *(float4*)(x + 4) = ((const float4*)p)[1];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = p[e];
   }
-  if (!cs) return make_float2(x0, x1);
-  const float2 c = *(const float2*)(cs + 2 * f);
-  return make_float2(x0 * c.x - x1 * c.y, x1 * c.x + x0 * c.y);
+}
+__device__ inline void load8(const bf16_t* p, bool vec, float (&x)[8]) {
+  bf16_t y[8];
+  if (vec) {
+    *(uint4*)y = *(const uint4*)p;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = p[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] = bf2f(y[e]);
+}
+__device__ inline void store8(float* p, bool vec, const float (&x)[8]) {
+  if (vec) {
+    ((float4*)p)[0] = *(const float4*)x;
+    ((float4*)p)[1] = *(const float4*)(x + 4);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = x[e];
+  }
+}
+__device__ inline void store8(bf16_t* p, bool vec, const float (&x)[8]) {
+  bf16_t y[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e]);
+  if (vec) {
+    *(uint4*)p = *(const uint4*)y;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = y[e];
+  }
+}
+// 8 codes of x s
+__device__ inline uint2 codes8(const float (&x)[8], float s) {
+  uint32_t w[2] = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) w[e >> 2] |= code_of(x[e] * s) << (8 * (e & 3));
+  return make_uint2(w[0], w[1]);
+}
+__device__ inline float amax8(float m, const float (&x)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (finite_f(x[e])) m = fmaxf(m, fabsf(x[e]));
+  return m;
+}
+
+// A lane's part of a head: dims f .. f + 7 (x) and f + hd/2 .. (y), hd/16 lanes a
+// head.  An optional RMS norm over the head, then the rotation of the pairs (f, f +
+// hd/2) by the table's angles of the position.
+template <int HD>
+__device__ inline void turn(float (&x)[8], float (&y)[8], const float* cs, const float* gain,
+                            float eps, int f) {
+  if (gain) {
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
+    const float r = 1.0f / sqrtf(group_sum<HD / 16>(ss) / (float)HD + eps);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      x[e] = x[e] * r * gain[f + e];
+      y[e] = y[e] * r * gain[f + HD / 2 + e];
+    }
+  }
+  if (!cs) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float2 c = *(const float2*)(cs + 2 * (f + e));
+    const float u = x[e] * c.x - y[e] * c.y;
+    y[e] = y[e] * c.x + x[e] * c.y;
+    x[e] = u;
+  }
 }
 
 // Workgroups [0, n_kv): one scale block (bf16: 16 tokens) of one head of one
 // sequence each; waves 0 and 1 take its keys, 2 and 3 its values.  A workgroup
-// owns all codes of its block, so it may change the block's scale.  Workgroups
-// from n_kv on: one row and query head per wave.
+// owns all codes of its block, so it may change the block's scale.  Its new rows stay
+// in registers (keys) and LDS (values, which change from token-major to
+// dimension-major there) between the search for the largest and the codes; blocks of
+// more than 64 tokens read them again.  Workgroups from n_kv on: query heads.  All
+// rows move 16 bytes a lane where they are aligned.
+//
+// Memory bounds it: 13000 rows of 48 heads, 64-token blocks, 4.1 TB/s read and
+// written (a copy of that size 4.6).
+constexpr int APP_T = 64;   // tokens of a pass
+constexpr int APP_QW = 16;  // query heads of a wave at head dim 128
+
 template <typename T, int HD, bool E4>
 __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int touched) {
-  constexpr int LT = HD / 2;   // lanes of a key or query row
-  constexpr int TP = 64 / LT;  // rows a wave holds at a time
+  constexpr int HL = HD / 16;                  // lanes of a key or query row
+  constexpr int TW = 64 / HL;                  // rows of a wave at a time
+  constexpr int KIT = APP_T / (2 * TW);        // key rows a lane
+  constexpr int VL = HD / 8, VW = 64 / VL;     // the same of values
+  constexpr int VIT = APP_T / (2 * VW);
   const PagedCache& c = a.cache;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int f = lane % LT, sub = lane / LT;
-  const int c0 = a.perm ? qkv_perm(f, HD) : f, c1 = a.perm ? qkv_perm(f + LT, HD) : f + LT;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int f = lane % HL * 8;
+  const int c0 = a.perm ? 2 * f : f, c1 = a.perm ? 2 * f + 8 : f + HD / 2;  // see qkv_perm
 
   if ((int)blockIdx.x >= n_kv) {
+    constexpr int QW = APP_QW * 128 / HD;  // query heads of a wave
+    const int per = (a.hq + QW - 1) / QW;
     const int job = ((int)blockIdx.x - n_kv) * 4 + wave;
-    const int r = job / ((a.hq + TP - 1) / TP);
-    const int h = job % ((a.hq + TP - 1) / TP) * TP + sub;
+    const int r = job / per, h0 = job % per * QW + lane / HL;
     if (r >= a.rows.rows) return;
+    float x[QW / TW][8], y[QW / TW][8];
+#pragma unroll
+    for (int i = 0; i < QW / TW; ++i) {
+      const T* src = (const T*)a.q + (size_t)r * a.ldq + (size_t)min(h0 + TW * i, a.hq - 1) * HD;
+      load8(src + c0, a.vec & 1, x[i]);
+      load8(src + c1, a.vec & 1, y[i]);
+    }
     const int b = seq_of(a.rows, r);
     if (b < 0) return;
     const SeqRows sr = seq_rows(a.rows, b);
     if (r - sr.r0 >= sr.n) return;
     const int p = first_pos(a.rows, b) + (r - sr.r0);
     const bool ok = p >= 0 && (!a.rope || p < a.rope_rows);
-    const T* src = (const T*)a.q + (size_t)r * a.ldq + (size_t)min(h, a.hq - 1) * HD;
-    float2 y = turn<LT>(ld1(src + c0), ld1(src + c1),
-                        a.rope && ok ? a.rope + (size_t)p * HD : nullptr, a.q_gain, a.eps, f);
-    if (!ok) y = make_float2(0.f, 0.f);
-    if (h < a.hq) {
+    const float* cs = a.rope && ok ? a.rope + (size_t)p * HD : nullptr;
+#pragma unroll
+    for (int i = 0; i < QW / TW; ++i) {
+      turn<HD>(x[i], y[i], cs, a.q_gain, a.eps, f);
+      if (!ok)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
+      const int h = h0 + TW * i;
+      if (h >= a.hq) continue;
       T* dst = (T*)a.q_out + (size_t)r * a.ldqo + (size_t)h * HD;
-      st1(dst + f, y.x);
-      st1(dst + f + LT, y.y);
+      store8(dst + f, a.vec & 2, x[i]);
+      store8(dst + f + HD / 2, a.vec & 2, y[i]);
     }
     return;
   }
 
+  __shared__ __align__(16) T s_v[APP_T][HD];
+  __shared__ float s_max[4];
   const int t = blockIdx.x % touched;
   const int h = blockIdx.x / touched % c.hkv;
   const int b = blockIdx.x / touched / c.hkv;
@@ -189,40 +281,79 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
   const int n0 = max(bs, pa), n1 = min(bs + block, pe);  // its new tokens
   if (n0 >= n1) return;
   const int pid = a.rows.table[(size_t)b * a.rows.table_ld + (bs >> c.lpage)];
+  const bool is_k = wave < 2;
+  const int w2 = wave & 1;
+  const int row_of = sr.r0 - p0;  // row of position p: row_of + p
+
+  // keys t0 .. of a pass, rotated; rows at or past n1 repeat the last
+  float x[KIT][8], y[KIT][8];
+  auto keys = [&](int t0) __attribute__((always_inline)) {
+    const T* src = (const T*)a.k + (size_t)h * HD;
+#pragma unroll
+    for (int i = 0; i < KIT; ++i) {
+      const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
+      if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+      const T* r = src + (size_t)(row_of + min(p, n1 - 1)) * a.ldk;
+      load8(r + c0, a.vec & 4, x[i]);
+      load8(r + c1, a.vec & 4, y[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < KIT; ++i) {
+      const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
+      if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+      turn<HD>(x[i], y[i], a.rope ? a.rope + (size_t)min(p, n1 - 1) * HD : nullptr, a.k_gain,
+               a.eps, f);
+    }
+  };
+  // values into LDS; returns the largest of this lane's
+  auto values = [&](int t0) __attribute__((always_inline)) {
+    const T* src = (const T*)a.v + (size_t)h * HD;
+    float m = 0.f;
+    float z[VIT][8];
+    const int d = lane % VL * 8;
+    // the packed order swaps groups of 8 dims
+    const int cd = a.perm ? (d < HD / 2 ? 2 * d : 2 * (d - HD / 2) + 8) : d;
+#pragma unroll
+    for (int i = 0; i < VIT; ++i) {
+      const int p = t0 + 2 * VW * i + VW * w2 + lane / VL;
+      if (t0 + 2 * VW * i + VW * w2 >= n1) break;
+      load8(src + (size_t)(row_of + min(p, n1 - 1)) * a.ldv + cd, a.vec & 8, z[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < VIT; ++i) {
+      const int q = 2 * VW * i + VW * w2 + lane / VL;
+      if (t0 + 2 * VW * i + VW * w2 >= n1) break;
+      m = amax8(m, z[i]);
+      store8(&s_v[q][d], true, z[i]);
+    }
+    return m;
+  };
+
+  const int passes = (n1 - n0 + APP_T - 1) / APP_T;
+  if (is_k) keys(n0);
+  float amax = is_k ? 0.f : values(n0);
   if (pid < 0 || pid >= c.n_pages) {
     if (a.rows.err && threadIdx.x == 0) a.rows.err[b] = 1;
     return;
   }
   const int s0 = bs & (c.page - 1);  // the block's first slot in its page
   const size_t head = (size_t)pid * c.hkv + h;
-  const bool is_k = wave < 2;
-  const int row_of = sr.r0 - p0;  // row of position p: row_of + p
-  const int d = threadIdx.x - 128;  // value waves: the thread's dimension
-  const T* src = (const T*)(is_k ? a.k : a.v) + (size_t)h * HD;
-  if (!is_k) src += a.perm && d < HD ? qkv_perm(d, HD) : min(d, HD - 1);
-  const size_t ld = is_k ? a.ldk : a.ldv;
-
   float s = 1.f, inv = 1.f, ratio = 1.f;
   if (E4) {
-    __shared__ float s_max[4];
     float* sp = (is_k ? c.k_scale : c.v_scale) + (head << (c.lpage - lblock)) + (s0 >> lblock);
     float s_old = n0 > bs ? *sp : 0.f;  // earlier tokens only
     if (!(s_old > 0.f && s_old <= FLT_MAX)) s_old = 0.f;
-    float amax = 0.f;
-    if (is_k) {
-      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
-        const int pp = min(p, n1 - 1);
-        const T* x = src + (size_t)(row_of + pp) * ld;
-        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
-                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
-        if (finite_f(y.x)) amax = fmaxf(amax, fabsf(y.x));
-        if (finite_f(y.y)) amax = fmaxf(amax, fabsf(y.y));
+    for (int u = 0; u < passes; ++u) {
+      if (u > 0) {
+        if (is_k) keys(n0 + APP_T * u);
+        else amax = fmaxf(amax, values(n0 + APP_T * u));
       }
-    } else if (d < HD) {
-      for (int p = n0; p < n1; ++p) {
-        const float y = ld1(src + (size_t)(row_of + p) * ld);
-        if (finite_f(y)) amax = fmaxf(amax, fabsf(y));
-      }
+      if (is_k)
+#pragma unroll
+        for (int i = 0; i < KIT; ++i) {
+          if (n0 + APP_T * u + 2 * TW * i + TW * w2 >= n1) break;
+          amax = amax8(amax8(amax, x[i]), y[i]);
+        }
     }
     amax = wave_max64(amax);
     if (lane == 0) s_max[wave] = amax;
@@ -231,67 +362,75 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
     inv = inv_pow2(s);
     ratio = s_old * inv;  // earlier codes are multiplied by it
     if ((threadIdx.x & 127) == 0) *sp = s;
+  } else {
+    __syncthreads();
   }
 
-  if (is_k) {
-    const size_t base = (head << c.lpage) * HD + (size_t)s0 * HD;
-    if (E4) {
-      uint8_t* kc = (uint8_t*)c.k + base;
-      if (n0 > bs && ratio != 1.f)
-        for (int i = wave * 64 + lane; i < (n0 - bs) * HD; i += 128)
-          kc[i] = (uint8_t)code_of(value_of(kc[i]) * ratio);
-      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
-        const int pp = min(p, n1 - 1);
-        const T* x = src + (size_t)(row_of + pp) * ld;
-        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
-                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
-        if (p < n1) {
-          uint8_t* dst = kc + (size_t)(p - bs) * HD;
-          dst[f] = (uint8_t)code_of(y.x * inv);
-          dst[f + LT] = (uint8_t)code_of(y.y * inv);
-        }
-      }
-    } else {
-      bf16_t* kc = (bf16_t*)c.k + base;
-      for (int p = n0 + wave * TP + sub; p - sub < n1; p += 2 * TP) {
-        const int pp = min(p, n1 - 1);
-        const T* x = src + (size_t)(row_of + pp) * ld;
-        const float2 y = turn<LT>(ld1(x + c0), ld1(x + c1),
-                                  a.rope ? a.rope + (size_t)pp * HD : nullptr, a.k_gain, a.eps, f);
-        if (p < n1) {
-          bf16_t* dst = kc + (size_t)(p - bs) * HD;
-          dst[f] = f2bf(y.x);
-          dst[f + LT] = f2bf(y.y);
-        }
-      }
+  for (int u = 0; u < passes; ++u) {
+    const int t0 = n0 + APP_T * u;
+    if (passes > 1) {  // the rows again
+      __syncthreads();
+      if (is_k) keys(t0);
+      else values(t0);
+      __syncthreads();
     }
-    return;
-  }
-  if (d >= HD) return;
-  for (int g0 = bs; g0 < n1; g0 += GRAN) {  // granules that the block's tokens reach
-    if (g0 + GRAN <= n0 && (!E4 || ratio == 1.f)) continue;
-    const size_t off = ((head << c.lpage) + (size_t)(s0 + g0 - bs)) * HD + (size_t)d * GRAN;
-    if (E4) {
-      uint8_t* vc = (uint8_t*)c.v + off;
-      uint32_t w[4];
-      *(uint4*)w = *(const uint4*)vc;
-#pragma unroll
-      for (int i = 0; i < GRAN; ++i) {
-        const int p = g0 + i;
-        uint32_t cd = (w[i / 4] >> (8 * (i % 4))) & 0xFFu;
-        if (p < n0) {
-          if (ratio != 1.f) cd = code_of(value_of(cd) * ratio);
-        } else if (p < n1) {
-          cd = code_of(ld1(src + (size_t)(row_of + p) * ld) * inv);
-        }
-        w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
+    if (is_k) {
+      const size_t base = (head << c.lpage) * HD + (size_t)s0 * HD;
+      if (E4 && u == 0 && n0 > bs && ratio != 1.f) {
+        uint8_t* kc = (uint8_t*)c.k + base;
+        for (int i = w2 * 64 + lane; i < (n0 - bs) * HD; i += 128)
+          kc[i] = (uint8_t)code_of(value_of(kc[i]) * ratio);
       }
-      *(uint4*)vc = *(const uint4*)w;
-    } else {
-      bf16_t* vc = (bf16_t*)c.v + off;
-      for (int i = 0; i < GRAN; ++i) {
-        const int p = g0 + i;
-        if (p >= n0 && p < n1) vc[i] = f2bf(ld1(src + (size_t)(row_of + p) * ld));
+#pragma unroll
+      for (int i = 0; i < KIT; ++i) {
+        const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
+        if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+        if (p >= n1) continue;
+        const size_t at = base + (size_t)(p - bs) * HD + f;
+        if (E4) {
+          *(uint2*)((uint8_t*)c.k + at) = codes8(x[i], inv);
+          *(uint2*)((uint8_t*)c.k + at + HD / 2) = codes8(y[i], inv);
+        } else {
+          store8((bf16_t*)c.k + at, true, x[i]);
+          store8((bf16_t*)c.k + at + HD / 2, true, y[i]);
+        }
+      }
+      continue;
+    }
+    const int d = threadIdx.x - 128;
+    if (d >= HD) continue;
+    const int t1 = min(t0 + APP_T, n1);
+    // granules that this pass reaches (the first also those of earlier tokens)
+    for (int g0 = u == 0 && ratio != 1.f ? bs : t0 & ~(GRAN - 1); g0 < t1; g0 += GRAN) {
+      const size_t off = ((head << c.lpage) + (size_t)(s0 + g0 - bs)) * HD + (size_t)d * GRAN;
+      if (E4) {
+        uint8_t* vc = (uint8_t*)c.v + off;
+        uint32_t w[4];
+        if (g0 < t0 || g0 + GRAN > t1) *(uint4*)w = *(const uint4*)vc;
+#pragma unroll
+        for (int i = 0; i < GRAN; ++i) {
+          const int p = g0 + i;
+          if (p >= t0 && p < t1) {
+            const uint32_t cd = code_of(ld1(&s_v[p - t0][d]) * inv);
+            w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
+          } else if (p < n0 && ratio != 1.f) {
+            const uint32_t cd = code_of(value_of((w[i / 4] >> (8 * (i % 4))) & 0xFFu) * ratio);
+            w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
+          }
+        }
+        *(uint4*)vc = *(const uint4*)w;
+      } else {
+        bf16_t* vc = (bf16_t*)c.v + off;
+        if (g0 >= t0 && g0 + GRAN <= t1) {
+          float z[2][8];
+#pragma unroll
+          for (int i = 0; i < GRAN; ++i) z[i >> 3][i & 7] = ld1(&s_v[g0 + i - t0][d]);
+          store8(vc, true, z[0]);
+          store8(vc + 8, true, z[1]);
+        } else {
+          for (int i = max(g0, t0) - g0; i < min(g0 + GRAN, t1) - g0; ++i)
+            vc[i] = f2bf(ld1(&s_v[g0 + i - t0][d]));
+        }
       }
     }
   }
@@ -1120,6 +1259,7 @@ __global__ __launch_bounds__(256, 2) void k_pg_chunk(PagedAttn a) {
     constexpr int buf = decltype(buf_)::value;
     put(buf ^ 1, t0 + 2 * KT > wmin);
     load(t0 + 2 * KT);
+    __builtin_amdgcn_sched_barrier(0);  // the loads leave before the products
     if (t0 < lmax) {
       const int4 ok = *(const int4*)s_ok[buf];
       const bool mask = !__all(t0 + KT <= lmin && ok.x && ok.y && ok.z && ok.w);
@@ -1269,14 +1409,19 @@ __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
 
 }  // namespace
 
-void paged_append(const PagedAppend& a, hipStream_t st) {
+void paged_append(const PagedAppend& a_, hipStream_t st) {
+  PagedAppend a = a_;
   const PagedCache& c = a.cache;
   const int block = c.kind == KS_E4M3 ? c.block : GRAN;
   const int touched = (a.rows.max_rows + block - 2) / block + 1;
   const int n_kv = a.rows.B * c.hkv * touched;
-  const int tp = 128 / c.hd;  // query heads of a wave
-  const int jobs = a.q ? a.rows.rows * ((a.hq + tp - 1) / tp) : 0;
+  const int qw = APP_QW * 128 / c.hd;
+  const int jobs = a.q ? a.rows.rows * ((a.hq + qw - 1) / qw) : 0;
   const dim3 grid(n_kv + (jobs + 3) / 4);
+  const size_t es = a.dtype == KS_BF16 ? 2 : 4;
+  auto al = [&](const void* p, size_t ld) { return (((uintptr_t)p | ld * es) & 15) == 0; };
+  a.vec = (al(a.q, a.ldq) ? 1 : 0) | (al(a.q_out, a.ldqo) ? 2 : 0) | (al(a.k, a.ldk) ? 4 : 0) |
+          (al(a.v, a.ldv) ? 8 : 0);
 #define KS_APP(T_, HD_, E_) \
   KS_LAUNCH((k_pg_append<T_, HD_, E_>), grid, dim3(256), 0, st, a, n_kv, touched)
 #define KS_APP_T(T_)                                                   \

@@ -343,6 +343,27 @@ def test_same_rows_again_and_no_queries(E):
     assert got is qc and torch.equal(ref, qc)
 
 
+@pytest.mark.parametrize("kind,dtype,hd,block", [("e4m3", "bf16", 128, 256), ("e4m3", "f32", 64, 128),
+                                                 ("bf16", "f32", 128, 16), ("e4m3", "bf16", 64, 64)])
+def test_append_long_blocks_and_unaligned_rows(E, kind, dtype, hd, block):
+    """Blocks of several passes, begun and ended anywhere; rows at addresses that are
+    no multiple of 16 bytes."""
+    x = Case(E, 2, 3, 1, hd, 256, block, kind, dtype, 2, seed=14)
+    for n, off in (([37, 300], 0), ([150, 9], 1), ([1, 1], 3), ([200, 130], 5), ([3, 0], 0)):
+        start, pos0 = np.cumsum([0] + n), x.len.copy()
+        r = int(start[-1])
+        (q, k, v), (fq, fk, fv) = x.rows(r, 1.0 + off)
+        pad = lambda t, h: torch.zeros(r * (h * hd + off) + 16, dtype=t.dtype, device="cuda")[
+            off:off + r * (h * hd + off)].view(r, h * hd + off)[:, :h * hd].view(r, h, hd)
+        k2, v2, q2 = pad(k, 1).copy_(k), pad(v, 1).copy_(v), pad(q, 3).copy_(q)
+        qo = E.paged_append(x.cache, i32(x.table), i32(start), i32(pos0), k2, v2, q=q2,
+                            rope=torch.from_numpy(x.rope).cuda(), q_out=pad(q, 3))
+        x.plain.append(x.table, start, pos0, fk, fv, x.rope)
+        x.len += n
+        x.check_queries(fq, qo, start, pos0, True)
+        x.check_cache()
+
+
 @pytest.mark.parametrize("std", [1e-40, 1e-33, 1e30])
 def test_magnitudes(E, std):
     """Scales down to 2^-100 and values near the float32 limits."""
