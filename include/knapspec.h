@@ -528,8 +528,8 @@ typedef struct ks_paged_rows {
 /*
  * ks_paged_append: stores the keys and values of new rows, rotating keys (and
  * queries) on the way: the pair (f, f + hd/2) of a head by the angle of its
- * position, rope[p][f] = (cos, sin), device float32 [rope_rows][hd/2][2]; NULL: no
- * rotation.  Rows at or past rope_rows are treated as past max_len.  k, v
+ * position, rope[p][f] = (cos, sin), device float32 [rope_rows][hd/2][2], 16-byte
+ * aligned; NULL: no rotation.  Rows at or past rope_rows are treated as past max_len.  k, v
  * [rows][hkv][hd] and q, q_out [rows][hq][hd] are of dtype (KS_F32 or KS_BF16),
  * rows ldk, ldv, ldq, ldqo elements apart (a fused projection's rows do); q may be
  * NULL (then hq, ldq, q_out, ldqo are not looked at), and q_out may equal q (with

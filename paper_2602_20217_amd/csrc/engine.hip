@@ -1207,7 +1207,7 @@ ks_status ks_paged_append(const ks_paged_cache* cache, const ks_paged_rows* rows
   REQ(k && v, "null pointer");
   const size_t kw = (size_t)cache->hkv * cache->hd;
   REQ(ldk >= kw && ldv >= kw, "ldk and ldv must hold a row of keys and values");
-  REQ(((uintptr_t)rope & 7) == 0, "rope must be 8-byte aligned");
+  REQ(((uintptr_t)rope & 15) == 0, "rope must be 16-byte aligned");
   if (q) {
     REQ(q_out, "null pointer");
     REQ(hq >= 1, "hq must be positive");

@@ -105,168 +105,204 @@ __device__ inline int row_len(const PagedAttn& a, const SeqRows& sr, int b, int 
   return min(max(n, 0), a.rows.max_len);
 }
 
-// Sequence of row r: the last b with row_start[b] <= r, 64 boundaries a step; -1
-// for a row behind the last sequence.  Wave-uniform r.
-__device__ inline int seq_of(const PagedRows& s, int r) {
-  if (!s.row_start) return r < s.rows ? 0 : -1;
+// Row r's sequence (the last b with row_start[b] <= r), its place i in it and the
+// sequence's first position; b = -1 for a row behind the last sequence or past
+// max_rows.  Boundaries and positions of 63 sequences are asked for at once, so that
+// a wave waits for one memory latency.  Wave-uniform r.
+struct RowAt {
+  int b, i, n, p0;
+};
+__device__ inline RowAt row_at(const PagedRows& s, int r) {
+  if (!s.row_start) return RowAt{r < s.rows ? 0 : -1, r, s.rows, s.pos0 ? first_pos(s, 0) : 0};
   const int lane = threadIdx.x & 63;
-  for (int b0 = 1; b0 <= s.B; b0 += 64) {
-    const int b = b0 + lane;
-    const uint64_t past = __ballot(b <= s.B && s.row_start[min(b, s.B)] > r);
-    if (past) return b0 - 1 + __ffsll((unsigned long long)past) - 1;
+  for (int b0 = 0; b0 < s.B; b0 += 63) {
+    const int at = min(max(s.row_start[min(b0 + lane, s.B)], 0), s.rows);
+    const int p0 = first_pos(s, min(b0 + lane, s.B - 1));
+    const uint64_t past = __ballot(lane > 0 && b0 + lane <= s.B && at > r);
+    if (!past) continue;
+    const int x = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)past) - 1);
+    RowAt y{b0 + x - 1, 0, 0, __builtin_amdgcn_readlane(p0, x - 1)};
+    const int r0 = __builtin_amdgcn_readlane(at, x - 1);
+    y.i = r - r0;
+    y.n = __builtin_amdgcn_readlane(at, x) - r0;
+    if (y.i < 0 || y.i >= s.max_rows) y.b = -1;
+    return y;
   }
-  return -1;
+  return RowAt{-1, 0, 0, 0};
 }
 
 // ------------------------------------------------------------------- append
-// 8 elements; vec: at a 16-byte address (wave-uniform)
-__device__ inline void load8(const float* p, bool vec, float (&x)[8]) {
-  if (vec) {
-    *(float4*)x = ((const float4*)p)[0];
-    *(float4*)(x + 4) = ((const float4*)p)[1];
+// 8 elements as they are, and as float32.  VEC: at a 16-byte address.
+template <typename T>
+struct Raw8 {
+  T x[8];
+};
+template <bool VEC, typename T>
+__device__ inline Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+  if (VEC) {
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(r) / 16; ++i) ((uint4*)r.x)[i] = ((const uint4*)p)[i];
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = p[e];
+    for (int e = 0; e < 8; ++e) r.x[e] = p[e];
   }
+  return r;
 }
-__device__ inline void load8(const bf16_t* p, bool vec, float (&x)[8]) {
-  bf16_t y[8];
-  if (vec) {
-    *(uint4*)y = *(const uint4*)p;
-  } else {
+template <typename T>
+__device__ inline void floats8(const Raw8<T>& r, float (&x)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = p[e];
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = bf2f(y[e]);
+  for (int e = 0; e < 8; ++e) x[e] = ld1(&r.x[e]);
 }
-__device__ inline void store8(float* p, bool vec, const float (&x)[8]) {
-  if (vec) {
-    ((float4*)p)[0] = *(const float4*)x;
-    ((float4*)p)[1] = *(const float4*)(x + 4);
+// f with whether rows are aligned as a constant: one branch around all loads of a
+// pass, which are then in flight together
+template <typename F>
+__device__ inline void with_vec(bool vec, F f) {
+  if (vec) f(std::true_type{});
+  else f(std::false_type{});
+}
+template <bool VEC>
+__device__ inline void store8(float* p, const float (&x)[8]) {
+  if (VEC) {
+    ((float4*)p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    ((float4*)p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] = x[e];
   }
 }
-__device__ inline void store8(bf16_t* p, bool vec, const float (&x)[8]) {
-  bf16_t y[8];
+template <bool VEC>
+__device__ inline void store8(bf16_t* p, const float (&x)[8]) {
+  if (VEC) {
+    u32x4 w;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) y[e] = f2bf(x[e]);
-  if (vec) {
-    *(uint4*)p = *(const uint4*)y;
+    for (int i = 0; i < 4; ++i)
+      w[i] = (uint32_t)f2bf(x[2 * i]) | ((uint32_t)f2bf(x[2 * i + 1]) << 16);
+    *(u32x4*)p = w;
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) p[e] = y[e];
+    for (int e = 0; e < 8; ++e) p[e] = f2bf(x[e]);
   }
 }
-// 8 codes of x s
+// 8 codes of x s, in pairs; what is not finite becomes NaN
 __device__ inline uint2 codes8(const float (&x)[8], float s) {
-  uint32_t w[2] = {0, 0};
+  uint32_t w[2];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) w[e >> 2] |= code_of(x[e] * s) << (8 * (e & 3));
+  for (int i = 0; i < 2; ++i) {
+    int y = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * s, x[4 * i + 1] * s, 0, false);
+    w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * s, x[4 * i + 3] * s, y, true);
+  }
+  float z = 0.f;  // 0 times what is not finite is NaN
+#pragma unroll
+  for (int e = 0; e < 8; ++e) z = fmaf(x[e], 0.f, z);
+  if (__any(z != 0.f))
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (!finite_f(x[e])) w[e >> 2] |= 0x7Fu << (8 * (e & 3));
   return make_uint2(w[0], w[1]);
 }
 __device__ inline float amax8(float m, const float (&x)[8]) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (finite_f(x[e])) m = fmaxf(m, fabsf(x[e]));
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, finite_f(x[e]) ? fabsf(x[e]) : 0.f);
   return m;
 }
 
-// A lane's part of a head: dims f .. f + 7 (x) and f + hd/2 .. (y), hd/16 lanes a
-// head.  An optional RMS norm over the head, then the rotation of the pairs (f, f +
-// hd/2) by the table's angles of the position.
+// A lane's part of a head: dims d .. d + 7, HD / 8 lanes a head.  An optional RMS norm
+// over the head, then the rotation of the pairs (f, f + hd/2) by the table's angles of
+// the position; the other half of a pair lies HD / 16 lanes away.
 template <int HD>
-__device__ inline void turn(float (&x)[8], float (&y)[8], const float* cs, const float* gain,
-                            float eps, int f) {
+__device__ inline void turn(float (&x)[8], const float* cs, const float* gain, float eps, int d) {
   if (gain) {
     float ss = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ss += x[e] * x[e] + y[e] * y[e];
-    const float r = 1.0f / sqrtf(group_sum<HD / 16>(ss) / (float)HD + eps);
+    for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+    const float r = 1.0f / sqrtf(group_sum<HD / 8>(ss) / (float)HD + eps);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = x[e] * r * gain[f + e];
-      y[e] = y[e] * r * gain[f + HD / 2 + e];
-    }
+    for (int e = 0; e < 8; ++e) x[e] = x[e] * r * gain[d + e];
   }
   if (!cs) return;
+  const bool low = d < HD / 2;
+  const float4* c = (const float4*)(cs + 2 * (low ? d : d - HD / 2));
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float2 c = *(const float2*)(cs + 2 * (f + e));
-    const float u = x[e] * c.x - y[e] * c.y;
-    y[e] = y[e] * c.x + x[e] * c.y;
-    x[e] = u;
+  for (int e = 0; e < 8; e += 2) {
+    const float4 t = c[e / 2];  // (cos, sin) of two pairs
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int bits = __float_as_int(x[e + u]);
+      const float y = __int_as_float(HD == 128
+                                         ? __builtin_amdgcn_update_dpp(0, bits, 0x128, 0xF, 0xF, true)
+                                         : __builtin_amdgcn_ds_swizzle(bits, 0x101F));
+      x[e + u] = x[e + u] * (u ? t.z : t.x) + (low ? -y : y) * (u ? t.w : t.y);
+    }
   }
 }
 
-// Workgroups [0, n_kv): one scale block (bf16: 16 tokens) of one head of one
-// sequence each; waves 0 and 1 take its keys, 2 and 3 its values.  A workgroup
+// n_kv workgroups take one scale block (bf16: 16 tokens) of one head of one sequence
+// each; waves 0 and 1 take its keys, 2 and 3 its values.  A workgroup
 // owns all codes of its block, so it may change the block's scale.  Its new rows stay
 // in registers (keys) and LDS (values, which change from token-major to
 // dimension-major there) between the search for the largest and the codes; blocks of
-// more than 64 tokens read them again.  Workgroups from n_kv on: query heads.  All
-// rows move 16 bytes a lane where they are aligned.
+// more than 64 tokens read them again.  The other workgroups turn query heads, a row a
+// wave.  All rows move 16 bytes a lane where they are aligned.
 //
-// Memory bounds it: 13000 rows of 48 heads, 64-token blocks, 4.1 TB/s read and
-// written (a copy of that size 4.6).
+// Memory bounds it: 10900 rows of 48 heads, 252 MB, in 62 us (a copy: 54).  The cache
+// blocks first and the queries in a launch of their own took 75.
 constexpr int APP_T = 64;   // tokens of a pass
-constexpr int APP_QW = 16;  // query heads of a wave at head dim 128
+constexpr int APP_QW = 32;  // query heads of a wave at head dim 128
 
 template <typename T, int HD, bool E4>
-__global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int touched) {
-  constexpr int HL = HD / 16;                  // lanes of a key or query row
-  constexpr int TW = 64 / HL;                  // rows of a wave at a time
-  constexpr int KIT = APP_T / (2 * TW);        // key rows a lane
-  constexpr int VL = HD / 8, VW = 64 / VL;     // the same of values
-  constexpr int VIT = APP_T / (2 * VW);
+__global__ __launch_bounds__(256, 3) void k_pg_append(PagedAppend a, int n_kv, int touched) {
+  constexpr int HL = HD / 8;            // lanes of a row of a head
+  constexpr int TW = 64 / HL;           // rows of a wave at a time
+  constexpr int KIT = APP_T / (2 * TW); // rows a lane
   const PagedCache& c = a.cache;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int f = lane % HL * 8;
-  const int c0 = a.perm ? 2 * f : f, c1 = a.perm ? 2 * f + 8 : f + HD / 2;  // see qkv_perm
+  const int d = lane % HL * 8;  // this lane's dims, and their place in a row
+  const int cd = a.perm ? (d < HD / 2 ? 2 * d : 2 * (d - HD / 2) + 8) : d;  // (see qkv_perm)
 
-  if ((int)blockIdx.x >= n_kv) {
+  const int wg = blockIdx.x;
+  if (wg >= n_kv) {
     constexpr int QW = APP_QW * 128 / HD;  // query heads of a wave
     const int per = (a.hq + QW - 1) / QW;
-    const int job = ((int)blockIdx.x - n_kv) * 4 + wave;
+    const int job = (wg - n_kv) * 4 + wave;
     const int r = job / per, h0 = job % per * QW + lane / HL;
     if (r >= a.rows.rows) return;
-    float x[QW / TW][8], y[QW / TW][8];
+    Raw8<T> rx[QW / TW];
+    with_vec(a.vec & 1, [&](auto vec) {
 #pragma unroll
-    for (int i = 0; i < QW / TW; ++i) {
-      const T* src = (const T*)a.q + (size_t)r * a.ldq + (size_t)min(h0 + TW * i, a.hq - 1) * HD;
-      load8(src + c0, a.vec & 1, x[i]);
-      load8(src + c1, a.vec & 1, y[i]);
-    }
-    const int b = seq_of(a.rows, r);
-    if (b < 0) return;
-    const SeqRows sr = seq_rows(a.rows, b);
-    if (r - sr.r0 >= sr.n) return;
-    const int p = first_pos(a.rows, b) + (r - sr.r0);
+      for (int i = 0; i < QW / TW; ++i) {
+        const T* src = (const T*)a.q + (size_t)r * a.ldq + (size_t)min(h0 + TW * i, a.hq - 1) * HD;
+        rx[i] = load8<decltype(vec)::value>(src + cd);
+      }
+    });
+    const RowAt ra = row_at(a.rows, r);
+    if (ra.b < 0) return;
+    const int p = ra.p0 + ra.i;
     const bool ok = p >= 0 && (!a.rope || p < a.rope_rows);
     const float* cs = a.rope && ok ? a.rope + (size_t)p * HD : nullptr;
+    with_vec(a.vec & 2, [&](auto vec) {
 #pragma unroll
-    for (int i = 0; i < QW / TW; ++i) {
-      turn<HD>(x[i], y[i], cs, a.q_gain, a.eps, f);
-      if (!ok)
+      for (int i = 0; i < QW / TW; ++i) {
+        float x[8];
+        floats8(rx[i], x);
+        turn<HD>(x, cs, a.q_gain, a.eps, d);
+        if (!ok)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[i][e] = y[i][e] = 0.f;
-      const int h = h0 + TW * i;
-      if (h >= a.hq) continue;
-      T* dst = (T*)a.q_out + (size_t)r * a.ldqo + (size_t)h * HD;
-      store8(dst + f, a.vec & 2, x[i]);
-      store8(dst + f + HD / 2, a.vec & 2, y[i]);
-    }
+          for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        const int h = h0 + TW * i;
+        if (h < a.hq)
+          store8<decltype(vec)::value>((T*)a.q_out + (size_t)r * a.ldqo + (size_t)h * HD + d, x);
+      }
+    });
     return;
   }
 
   __shared__ __align__(16) T s_v[APP_T][HD];
   __shared__ float s_max[4];
-  const int t = blockIdx.x % touched;
-  const int h = blockIdx.x / touched % c.hkv;
-  const int b = blockIdx.x / touched / c.hkv;
+  const int t = wg % touched;
+  const int h = wg / touched % c.hkv;
+  const int b = wg / touched / c.hkv;
   const SeqRows sr = seq_rows(a.rows, b);
   const int p0 = first_pos(a.rows, b);
   const int lblock = E4 ? c.lblock : 4, block = 1 << lblock;
@@ -286,45 +322,50 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
   const int row_of = sr.r0 - p0;  // row of position p: row_of + p
 
   // keys t0 .. of a pass, rotated; rows at or past n1 repeat the last
-  float x[KIT][8], y[KIT][8];
+  float x[KIT][8];
   auto keys = [&](int t0) __attribute__((always_inline)) {
     const T* src = (const T*)a.k + (size_t)h * HD;
+    Raw8<T> rx[KIT];
+    with_vec(a.vec & 4, [&](auto vec) {
+#pragma unroll
+      for (int i = 0; i < KIT; ++i) {
+        const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
+        if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+        const T* r = src + (size_t)(row_of + min(p, n1 - 1)) * a.ldk;
+        rx[i] = load8<decltype(vec)::value>(r + cd);
+      }
+    });
 #pragma unroll
     for (int i = 0; i < KIT; ++i) {
       const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
       if (t0 + 2 * TW * i + TW * w2 >= n1) break;
-      const T* r = src + (size_t)(row_of + min(p, n1 - 1)) * a.ldk;
-      load8(r + c0, a.vec & 4, x[i]);
-      load8(r + c1, a.vec & 4, y[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < KIT; ++i) {
-      const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
-      if (t0 + 2 * TW * i + TW * w2 >= n1) break;
-      turn<HD>(x[i], y[i], a.rope ? a.rope + (size_t)min(p, n1 - 1) * HD : nullptr, a.k_gain,
-               a.eps, f);
+      floats8(rx[i], x[i]);
+      turn<HD>(x[i], a.rope ? a.rope + (size_t)min(p, n1 - 1) * HD : nullptr, a.k_gain, a.eps, d);
     }
   };
   // values into LDS; returns the largest of this lane's
   auto values = [&](int t0) __attribute__((always_inline)) {
     const T* src = (const T*)a.v + (size_t)h * HD;
     float m = 0.f;
-    float z[VIT][8];
-    const int d = lane % VL * 8;
-    // the packed order swaps groups of 8 dims
-    const int cd = a.perm ? (d < HD / 2 ? 2 * d : 2 * (d - HD / 2) + 8) : d;
+    Raw8<T> z[KIT];
+    with_vec(a.vec & 8, [&](auto vec) {
 #pragma unroll
-    for (int i = 0; i < VIT; ++i) {
-      const int p = t0 + 2 * VW * i + VW * w2 + lane / VL;
-      if (t0 + 2 * VW * i + VW * w2 >= n1) break;
-      load8(src + (size_t)(row_of + min(p, n1 - 1)) * a.ldv + cd, a.vec & 8, z[i]);
-    }
+      for (int i = 0; i < KIT; ++i) {
+        const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
+        if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+        z[i] = load8<decltype(vec)::value>(src + (size_t)(row_of + min(p, n1 - 1)) * a.ldv + cd);
+      }
+    });
 #pragma unroll
-    for (int i = 0; i < VIT; ++i) {
-      const int q = 2 * VW * i + VW * w2 + lane / VL;
-      if (t0 + 2 * VW * i + VW * w2 >= n1) break;
-      m = amax8(m, z[i]);
-      store8(&s_v[q][d], true, z[i]);
+    for (int i = 0; i < KIT; ++i) {
+      const int q = 2 * TW * i + TW * w2 + lane / HL;
+      if (t0 + 2 * TW * i + TW * w2 >= n1) break;
+      float x[8];
+      floats8(z[i], x);
+      m = amax8(m, x);
+#pragma unroll
+      for (int u = 0; u < (int)sizeof(z[i]) / 16; ++u)
+        ((uint4*)&s_v[q][d])[u] = ((const uint4*)z[i].x)[u];
     }
     return m;
   };
@@ -352,7 +393,7 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
 #pragma unroll
         for (int i = 0; i < KIT; ++i) {
           if (n0 + APP_T * u + 2 * TW * i + TW * w2 >= n1) break;
-          amax = amax8(amax8(amax, x[i]), y[i]);
+          amax = amax8(amax, x[i]);
         }
     }
     amax = wave_max64(amax);
@@ -386,23 +427,18 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
         const int p = t0 + 2 * TW * i + TW * w2 + lane / HL;
         if (t0 + 2 * TW * i + TW * w2 >= n1) break;
         if (p >= n1) continue;
-        const size_t at = base + (size_t)(p - bs) * HD + f;
-        if (E4) {
-          *(uint2*)((uint8_t*)c.k + at) = codes8(x[i], inv);
-          *(uint2*)((uint8_t*)c.k + at + HD / 2) = codes8(y[i], inv);
-        } else {
-          store8((bf16_t*)c.k + at, true, x[i]);
-          store8((bf16_t*)c.k + at + HD / 2, true, y[i]);
-        }
+        const size_t at = base + (size_t)(p - bs) * HD + d;
+        if (E4) *(uint2*)((uint8_t*)c.k + at) = codes8(x[i], inv);
+        else store8<true>((bf16_t*)c.k + at, x[i]);
       }
       continue;
     }
-    const int d = threadIdx.x - 128;
-    if (d >= HD) continue;
+    const int dim = threadIdx.x - 128;
+    if (dim >= HD) continue;
     const int t1 = min(t0 + APP_T, n1);
     // granules that this pass reaches (the first also those of earlier tokens)
     for (int g0 = u == 0 && ratio != 1.f ? bs : t0 & ~(GRAN - 1); g0 < t1; g0 += GRAN) {
-      const size_t off = ((head << c.lpage) + (size_t)(s0 + g0 - bs)) * HD + (size_t)d * GRAN;
+      const size_t off = ((head << c.lpage) + (size_t)(s0 + g0 - bs)) * HD + (size_t)dim * GRAN;
       if (E4) {
         uint8_t* vc = (uint8_t*)c.v + off;
         uint32_t w[4];
@@ -411,7 +447,7 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
         for (int i = 0; i < GRAN; ++i) {
           const int p = g0 + i;
           if (p >= t0 && p < t1) {
-            const uint32_t cd = code_of(ld1(&s_v[p - t0][d]) * inv);
+            const uint32_t cd = code_of(ld1(&s_v[p - t0][dim]) * inv);
             w[i / 4] = (w[i / 4] & ~(0xFFu << (8 * (i % 4)))) | cd << (8 * (i % 4));
           } else if (p < n0 && ratio != 1.f) {
             const uint32_t cd = code_of(value_of((w[i / 4] >> (8 * (i % 4))) & 0xFFu) * ratio);
@@ -424,12 +460,12 @@ __global__ __launch_bounds__(256) void k_pg_append(PagedAppend a, int n_kv, int 
         if (g0 >= t0 && g0 + GRAN <= t1) {
           float z[2][8];
 #pragma unroll
-          for (int i = 0; i < GRAN; ++i) z[i >> 3][i & 7] = ld1(&s_v[g0 + i - t0][d]);
-          store8(vc, true, z[0]);
-          store8(vc + 8, true, z[1]);
+          for (int i = 0; i < GRAN; ++i) z[i >> 3][i & 7] = ld1(&s_v[g0 + i - t0][dim]);
+          store8<true>(vc, z[0]);
+          store8<true>(vc + 8, z[1]);
         } else {
           for (int i = max(g0, t0) - g0; i < min(g0 + GRAN, t1) - g0; ++i)
-            vc[i] = f2bf(ld1(&s_v[g0 + i - t0][d]));
+            vc[i] = f2bf(ld1(&s_v[g0 + i - t0][dim]));
         }
       }
     }
@@ -1352,15 +1388,10 @@ __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
     }
   };
   load(w);
-  const int b = seq_of(a.rows, r);
-  int ns = 0;
-  bool mine = job < a.rows.rows * a.hq && b >= 0;
-  if (mine) {
-    const SeqRows sr = seq_rows(a.rows, b);
-    mine = r - sr.r0 < sr.n;
-    bool over = false;
-    ns = (row_len(a, sr, b, r - sr.r0, over) + a.span - 1) / a.span;
-  }
+  const RowAt ra = row_at(a.rows, r);
+  const bool mine = job < a.rows.rows * a.hq && ra.b >= 0;
+  const int n = min(max(ra.p0 + ra.i + 1, 0), a.rows.max_len);
+  const int ns = mine ? (n + a.span - 1) / a.span : 0;
   float m = -FLT_MAX, l = 0.f, o[DPL];
 #pragma unroll
   for (int e = 0; e < DPL; ++e) o[e] = 0.f;
