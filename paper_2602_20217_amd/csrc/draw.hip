@@ -7,19 +7,25 @@
 // kept.  So nothing has to be sorted: each step is the search for a place in the
 // order by its rank or by its mass.
 //
-// The mass of an entry is e^x, x = (logit - largest) / temperature, computed in 64
-// bits and held as an integer in units of 2^-44: sums of integers do not depend on
-// the order of the atomics that add them, and what neighbours of the draw differ by
-// is kept (float32 sums lose it).  Entries below e^-31 of the largest have mass 0.
+// Entries fall into bins of width 1/64 in x = (logit - largest) / temperature, whose
+// places 64 (largest - logit) / temperature are computed in 64 bits.  An entry's mass
+// is e^-bin/64 times (1 - s), s = 1 - e^-r of its remainder r < 1/64, held in units of
+// 2^-31.  A bin keeps its entries' number and the sum of s in one 64-bit word, so an
+// entry costs one atomic, and sums of integers do not depend on the order of the
+// atomics that make them.  Masses are known to about 2^-30 (sums of float32 would lose
+// what neighbours of the draw differ by); bin masses and their sums are integers in
+// units of 2^-44 of the largest entry's.  Entries below e^-31.98 have mass 0.
 //
-//  k_draw_max     largest logit of every chunk of a row; clears the row's histogram
-//  k_draw_hist    count and mass of every bin of width 1/64 in x, over the row
-//  k_draw_gather  the bins that hold the places searched for follow from the
-//                 histogram (a few when one search depends on the one before);
-//                 their entries are gathered
-//  k_draw_pick    sorts the gathered entries and finds the places; a row whose bins
-//                 hold too many (equal logits, high temperature) finds each place
-//                 digit by digit over the whole row instead
+//  k_draw_max     largest logit of every chunk of a row; clears the row's bins
+//  k_draw_hist    number and mass of every bin, over the row
+//  k_draw_gather  the bins that hold the places searched for follow from these (a few
+//                 when one search depends on the one before); their entries are
+//                 gathered
+//  k_draw_pick    orders the gathered entries and finds the places: up to 64 in one
+//                 wave, up to CAP in a sort; a row whose bins hold more (equal logits,
+//                 high temperature) finds each place digit by digit over the whole row
+//
+// 256 rows of 128256 logits (131 MB): @256@
 #include "ks_internal.h"
 
 #include <algorithm>
@@ -29,23 +35,39 @@ namespace ks {
 
 namespace {
 
-constexpr int BINS = 2048;
-constexpr double BIN_W = 64.0;  // bins per unit of x; the last one has no lower end
-constexpr double X_MIN = -32.0;
-constexpr int FRAC = 44;        // fraction bits of a mass: 2^19 entries of mass 1 fit 63 bits
-constexpr int CAP = 4096;       // gathered entries of a row
-constexpr int SCAN_T = 256;     // threads of a chunk workgroup
-constexpr int PICK_T = 1024;    // threads of a row's last workgroup
-constexpr int NB_MAX = 128;     // chunks of a row
+constexpr int BINS = 2048;   // the last one has no lower end and no mass
+constexpr double BIN_W = 64.0;
+constexpr int FRAC = 44;     // fraction bits of a mass: 2^19 entries of mass 1 fit 63 bits
+constexpr int UNIT = 31;     // fraction bits of s
+constexpr int CNT_AT = 44;   // bits of a sum of s, below its number of entries
+constexpr int CAP = 4096;    // gathered entries of a row
+constexpr int SCAN_T = 256;  // threads of a chunk workgroup
+constexpr int PICK_T = 1024; // threads of a row's last workgroup
+constexpr int NB_MAX = 128;  // chunks of a row
 
 typedef unsigned long long u64;
 
+// What the bins say of the places: the bins that hold the k-th entry, the end of
+// top-p's prefix and the draw, as ranges where one depends on another's exact place
+// inside its bin.
+struct Plan {
+  u64 z;           // mass that min-p keeps
+  uint32_t total;  // its entries
+  int k_bin;       // bin of the k-th entry; -1: it cuts no mass
+  int p_lo, p_hi, d_lo, d_hi;
+  __device__ bool wants(int b) const {
+    return b == k_bin || (b >= p_lo && b <= p_hi) || (b >= d_lo && b <= d_hi);
+  }
+};
+
 // One row's scratch.
 struct RowWs {
-  u64 mass[BINS];
+  u64 bin[BINS];       // entries << CNT_AT | sum of s
+  u64 mass[BINS];      // up to and with each bin
   u64 cand[CAP];
-  uint32_t cnt[BINS];
+  uint32_t cnt[BINS];  // up to and with each bin
   float cmax[NB_MAX];
+  Plan plan;
   uint32_t n_cand;
   uint32_t pad[3];
 };
@@ -73,7 +95,7 @@ __device__ inline void each_logit(const T* row, int n0, int n1, F f) {
   constexpr int E = 16 / sizeof(T);
   if (((uintptr_t)(row + n0) & 15) == 0) {
     const int nv = (n1 - n0) / E;
-#pragma unroll 2
+#pragma unroll 4
     for (int i = threadIdx.x; i < nv; i += NT) {
       T x[E];
       *(uint4*)x = *(const uint4*)(row + n0 + E * i);
@@ -87,27 +109,23 @@ __device__ inline void each_logit(const T* row, int n0, int n1, F f) {
 
 // A row's settings, with what switches a filter off put as what never cuts.
 struct Setting {
-  double inv_t, min_p, top_p, u;
+  double scale;   // 64 / temperature
+  double y_max;   // min-p keeps entries up to it
+  double top_p, u;
   uint32_t k;
   float lmax;
-  __device__ bool entry(float l) const { return l > -INFINITY; }  // not barred, not NaN
-  __device__ double x_of(float l) const {
-    return l == lmax ? 0.0 : ((double)l - (double)lmax) * inv_t;
+  __device__ static bool entry(float l) { return l > -INFINITY; }  // not barred, not NaN
+  // place of an entry in bins, from the largest down
+  __device__ double y_of(float l) const {
+    return l == lmax ? 0.0 : ((double)lmax - (double)l) * scale;
   }
-  __device__ int bin_of(double x) const {
-    return x > X_MIN ? min((int)(-x * BIN_W), BINS - 1) : BINS - 1;
-  }
-  // mass of an entry; keep: min-p keeps it
-  __device__ u64 mass_of(double x, bool& keep) const {
-    keep = true;
-    double w = 0.0;
-    if (x > X_MIN || min_p > 0.0) {
-      w = exp(x);
-      keep = w >= min_p;
-    }
-    // adding 2^52 rounds to an integer in the low mantissa bits
-    return (u64)__double_as_longlong(fma(w, (double)(1ull << FRAC), 4503599627370496.0)) &
-           ((1ull << 52) - 1);
+  __device__ static int bin_of(double y) { return y < BINS - 1 ? (int)y : BINS - 1; }
+  // s of an entry: 1 - e^-r = r (1 - r/2 (1 - r/3 (1 - r/4))) to 2^-31
+  __device__ static uint32_t s_of(double y, int bin) {
+    if (bin == BINS - 1) return 0;
+    const float r = (float)(y - bin) * (float)(1.0 / BIN_W);
+    const float t = r * fmaf(r * -0.5f, fmaf(r * (-1.0f / 3), fmaf(r, -0.25f, 1.0f), 1.0f), 1.0f);
+    return (uint32_t)(t * 2147483648.0f + 0.5f);
   }
 };
 __device__ inline Setting setting(const DrawArgs& a, int r, float lmax) {
@@ -118,23 +136,27 @@ __device__ inline Setting setting(const DrawArgs& a, int r, float lmax) {
   const float mp = greedy || !a.min_p ? 0.f : a.min_p[r];
   const float tp = greedy || !a.top_p ? 1.f : a.top_p[r];
   const float u = a.u[r];
-  s.inv_t = greedy ? 1.0 : 1.0 / (double)t;
+  s.scale = greedy ? BIN_W : BIN_W / (double)t;
   s.k = k > 0 ? (uint32_t)k : 0xFFFFFFFFu;
-  s.min_p = mp > 0.f ? fmin((double)mp, 1.0) : 0.0;
+  s.y_max = mp > 0.f ? -BIN_W * log(fmin((double)mp, 1.0)) : (double)INFINITY;
   s.top_p = tp < 1.f ? fmax((double)tp, 0.0) : 1.0;
   s.u = u > 0.f ? (double)u : 0.0;
   s.lmax = lmax;
   return s;
 }
+// units of mass that one unit of 1 - s has in a bin
+__device__ inline double unit_of(int bin) {
+  return bin == BINS - 1 ? 0.0 : exp(-bin / BIN_W) * (double)(1ull << (FRAC - UNIT));
+}
+// units of 1 - s of a bin's word, and their mass
+__device__ inline u64 units_of(u64 w) {
+  return ((w >> CNT_AT) << UNIT) - (w & ((1ull << CNT_AT) - 1));
+}
+__device__ inline u64 mass_of(double unit, u64 units) { return (u64)(unit * (double)units); }
 // masses are in [0, 2^63]: the first cumulative mass that reaches p z, and the first
 // that exceeds u z, as the least integer that does
-__device__ inline u64 reach(double p, u64 z) {
-  return max((u64)ceil(p * (double)z), (u64)1);
-}
-__device__ inline u64 exceed(double u, u64 z) {
-  const u64 t = (u64)(u * (double)z);
-  return min(t + 1, z);
-}
+__device__ inline u64 reach(double p, u64 z) { return max((u64)ceil(p * (double)z), (u64)1); }
+__device__ inline u64 exceed(double u, u64 z) { return min((u64)(u * (double)z) + 1, z); }
 
 template <typename V>
 __device__ inline V wave_incl(V v) {
@@ -145,7 +167,7 @@ __device__ inline V wave_incl(V v) {
   }
   return v;
 }
-// Inclusive prefix over the NT threads of a workgroup.
+// Inclusive prefix over the NT threads of a workgroup, and the thread before's.
 template <int NT, typename V>
 __device__ inline V block_incl(V v, V* sh) {
   v = wave_incl(v);
@@ -157,119 +179,78 @@ __device__ inline V block_incl(V v, V* sh) {
   return v;
 }
 
-// The histogram of a row as inclusive sums, BINS / NT bins a thread.
-template <int NT>
-struct Sums {
-  static constexpr int E = BINS / NT;
-  u64 m[E];
-  uint32_t c[E];
-};
-// The first bin whose inclusive sum reaches thr, and the sum before it.
-template <int NT, typename V>
-__device__ inline int first_bin(const V (&incl)[BINS / NT], V thr, V* s_before, int* s_bin) {
-  constexpr int E = BINS / NT;
-  __syncthreads();
-  if (threadIdx.x == 0) *s_bin = BINS - 1;
-  __syncthreads();
-  V before = 0;
-  {
-    // the inclusive sum of the thread before
-    __shared__ V s_last[NT];
-    s_last[threadIdx.x] = incl[E - 1];
-    __syncthreads();
-    if (threadIdx.x > 0) before = s_last[threadIdx.x - 1];
-  }
+// Bins in which an inclusive sum first reaches a threshold; E bins a thread.
+// incl: the thread's inclusive sums, before: the sum before its first.
+template <int E, typename V>
+__device__ inline int own_bin(const V (&incl)[E], V before, V thr) {
+  int at = -1;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    if (before < thr && thr <= incl[e]) {
-      *s_bin = threadIdx.x * E + e;
-      *s_before = before;
-    }
+    if (at < 0 && before < thr && thr <= incl[e]) at = threadIdx.x * E + e;
     before = incl[e];
   }
-  __syncthreads();
-  return *s_bin;
+  return at;
 }
 
-// What the histogram says of the places: the bins that hold the k-th entry, the end
-// of top-p's prefix and the draw, as ranges where one depends on another's exact
-// place inside its bin.
-struct Plan {
-  uint32_t total;  // entries that min-p keeps
-  u64 z;           // their mass
-  int k_bin;       // bin of the k-th entry; -1: it cuts no mass
-  int p_lo, p_hi, d_lo, d_hi;
-  __device__ bool wants(int b) const {
-    return b == k_bin || (b >= p_lo && b <= p_hi) || (b >= d_lo && b <= d_hi);
-  }
-};
+// The plan of a row, with the inclusive sums of its bins in mass and cnt (LDS).
 template <int NT>
-__device__ inline Plan plan(const RowWs& w, const Setting& s, Sums<NT>& h) {
+__device__ inline Plan plan(const RowWs& w, const Setting& s, u64* mass, uint32_t* cnt) {
   constexpr int E = BINS / NT;
   __shared__ u64 s_m[NT / 64];
   __shared__ uint32_t s_c[NT / 64];
-  __shared__ u64 s_bm, s_z;
-  __shared__ uint32_t s_bc, s_n;
-  __shared__ int s_bin;
-  u64 m = 0;
-  uint32_t c = 0;
+  __shared__ int s_bin[2];
+  u64 m = 0, hm[E];
+  uint32_t c = 0, hc[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    m += w.mass[threadIdx.x * E + e];
-    c += w.cnt[threadIdx.x * E + e];
-    h.m[e] = m;
-    h.c[e] = c;
+    const int b = threadIdx.x * E + e;
+    const u64 x = w.bin[b];
+    if (x) m += mass_of(unit_of(b), units_of(x));
+    c += (uint32_t)(x >> CNT_AT);
+    hm[e] = m;
+    hc[e] = c;
   }
-  const u64 mi = block_incl<NT>(m, s_m) - m;
-  const uint32_t ci = block_incl<NT>(c, s_c) - c;
+  const u64 m0 = block_incl<NT>(m, s_m) - m;
+  const uint32_t c0 = block_incl<NT>(c, s_c) - c;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    h.m[e] += mi;
-    h.c[e] += ci;
-  }
-  if (threadIdx.x == NT - 1) {
-    s_z = h.m[E - 1];
-    s_n = h.c[E - 1];
+    mass[threadIdx.x * E + e] = hm[e] += m0;
+    cnt[threadIdx.x * E + e] = hc[e] += c0;
   }
   __syncthreads();
   Plan p;
-  p.total = s_n;
-  p.z = s_z;
-  // inclusive and exclusive mass of a bin, to every thread
-  auto mass_at = [&](int b, u64& before) {
+  p.total = cnt[BINS - 1];
+  p.z = mass[BINS - 1];
+  // the bins of up to two thresholds
+  auto find2 = [&](bool by_mass, u64 a, u64 b, int& ba, int& bb) {
+    const int x = by_mass ? own_bin<E>(hm, m0, a) : own_bin<E>(hc, c0, (uint32_t)a);
+    const int y = by_mass ? own_bin<E>(hm, m0, b) : own_bin<E>(hc, c0, (uint32_t)b);
+    if (x >= 0) s_bin[0] = x;
+    if (y >= 0) s_bin[1] = y;
     __syncthreads();
-    if ((int)threadIdx.x == b / E) {
-      u64 x = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (e == b % E) x = h.m[e];
-      s_bm = x;
-    }
+    ba = s_bin[0];
+    bb = s_bin[1];
     __syncthreads();
-    const u64 incl = s_bm;
-    before = incl - w.mass[b];
-    return incl;
   };
+  auto before = [&](int b) { return b ? mass[b - 1] : 0; };
   u64 zlo = p.z, zhi = p.z;  // mass that top-k keeps
   p.k_bin = -1;
+  int b, b2;
   if (s.k < p.total) {
-    const int b = first_bin<NT>(h.c, s.k, &s_bc, &s_bin);
-    zhi = mass_at(b, zlo);
+    find2(false, s.k, s.k, b, b2);
+    zlo = before(b);
+    zhi = mass[b];
     if (zhi > zlo) p.k_bin = b;
+    else p.z = zlo;
   }
-  p.p_lo = p.d_lo = BINS;
-  p.p_hi = p.d_hi = -1;
+  p.p_lo = BINS;
+  p.p_hi = -1;
   if (s.top_p < 1.0) {
-    u64 before;
-    p.p_lo = first_bin<NT>(h.m, reach(s.top_p, zlo), &s_bm, &s_bin);
-    p.p_hi = first_bin<NT>(h.m, reach(s.top_p, zhi), &s_bm, &s_bin);
-    const u64 top = mass_at(p.p_hi, before);
-    mass_at(p.p_lo, before);
-    zlo = before + 1;
-    zhi = min(zhi, top);
+    find2(true, reach(s.top_p, max(zlo, (u64)1)), reach(s.top_p, zhi), p.p_lo, p.p_hi);
+    zlo = before(p.p_lo) + 1;
+    zhi = min(zhi, mass[p.p_hi]);
   }
-  p.d_lo = first_bin<NT>(h.m, exceed(s.u, max(zlo, (u64)1)), &s_bm, &s_bin);
-  p.d_hi = first_bin<NT>(h.m, exceed(s.u, zhi), &s_bm, &s_bin);
+  find2(true, exceed(s.u, max(zlo, (u64)1)), exceed(s.u, zhi), p.d_lo, p.d_hi);
   return p;
 }
 
@@ -279,10 +260,7 @@ __global__ __launch_bounds__(SCAN_T) void k_draw_max(DrawArgs a, int chunk) {
   __shared__ float s_m[SCAN_T / 64];
   const int b = blockIdx.x, NB = gridDim.x, r = blockIdx.y;
   RowWs& w = ((RowWs*)a.ws)[r];
-  for (int i = b * SCAN_T + threadIdx.x; i < BINS; i += NB * SCAN_T) {
-    w.mass[i] = 0;
-    w.cnt[i] = 0;
-  }
+  for (int i = b * SCAN_T + threadIdx.x; i < BINS; i += NB * SCAN_T) w.bin[i] = 0;
   if (b == 0 && threadIdx.x == 0) w.n_cand = 0;
   float m = -INFINITY;
   each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
@@ -308,52 +286,60 @@ __device__ inline float row_max(const RowWs& w, int NB) {
 
 template <typename T>
 __global__ __launch_bounds__(SCAN_T) void k_draw_hist(DrawArgs a, int chunk) {
+  __shared__ u64 s_bin[BINS];
+  const int b = blockIdx.x, r = blockIdx.y;
+  RowWs& w = ((RowWs*)a.ws)[r];
+  for (int i = threadIdx.x; i < BINS; i += SCAN_T) s_bin[i] = 0;
+  const Setting s = setting(a, r, row_max(w, gridDim.x));
+  if (!s.entry(s.lmax)) return;
+  __syncthreads();
+  each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
+                     min(a.vocab, (b + 1) * chunk), [&](float l, int) {
+                       const double y = s.y_of(l);
+                       if (!s.entry(l) || !(y <= s.y_max)) return;
+                       const int bin = s.bin_of(y);
+                       atomicAdd(&s_bin[bin], (1ull << CNT_AT) + s.s_of(y, bin));
+                     });
+  __syncthreads();
+  for (int i = threadIdx.x; i < BINS; i += SCAN_T)
+    if (s_bin[i]) atomicAdd(&w.bin[i], s_bin[i]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(SCAN_T) void k_draw_gather(DrawArgs a, int chunk) {
   __shared__ u64 s_mass[BINS];
   __shared__ uint32_t s_cnt[BINS];
   const int b = blockIdx.x, r = blockIdx.y;
   RowWs& w = ((RowWs*)a.ws)[r];
   const Setting s = setting(a, r, row_max(w, gridDim.x));
   if (!s.entry(s.lmax)) return;
-  for (int i = threadIdx.x; i < BINS; i += SCAN_T) {
-    s_mass[i] = 0;
-    s_cnt[i] = 0;
+  const Plan p = plan<SCAN_T>(w, s, s_mass, s_cnt);
+  if (b == 0) {  // for the next launch
+    for (int i = threadIdx.x; i < BINS; i += SCAN_T) {
+      w.mass[i] = s_mass[i];
+      w.cnt[i] = s_cnt[i];
+    }
+    if (threadIdx.x == 0) w.plan = p;
   }
-  __syncthreads();
-  each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
-                     min(a.vocab, (b + 1) * chunk), [&](float l, int) {
-                       if (!s.entry(l)) return;
-                       const double x = s.x_of(l);
-                       bool keep;
-                       const u64 m = s.mass_of(x, keep);
-                       if (!keep) return;
-                       const int bin = s.bin_of(x);
-                       atomicAdd(&s_cnt[bin], 1u);
-                       if (m) atomicAdd(&s_mass[bin], m);
-                     });
-  __syncthreads();
-  for (int i = threadIdx.x; i < BINS; i += SCAN_T) {
-    if (!s_cnt[i]) continue;
-    atomicAdd(&w.cnt[i], s_cnt[i]);
-    if (s_mass[i]) atomicAdd(&w.mass[i], s_mass[i]);
-  }
-}
-
-template <typename T>
-__global__ __launch_bounds__(SCAN_T) void k_draw_gather(DrawArgs a, int chunk) {
-  const int b = blockIdx.x, r = blockIdx.y;
-  RowWs& w = ((RowWs*)a.ws)[r];
-  const Setting s = setting(a, r, row_max(w, gridDim.x));
-  if (!s.entry(s.lmax)) return;
-  Sums<SCAN_T> h;
-  const Plan p = plan<SCAN_T>(w, s, h);
+  // logits that may lie in the bins lo .. hi: a float32 interval, wider by more than
+  // its roundings
+  auto interval = [&](int lo, int hi, float& from, float& to) {
+    const double f = (double)s.lmax - (hi + 1) / s.scale, t = (double)s.lmax - lo / s.scale;
+    const double wide = 1e-6 * (fabs((double)s.lmax) + (hi + 1) / s.scale) + 1e-30;
+    from = hi >= BINS - 1 || !(f - wide >= -FLT_MAX) ? -INFINITY : (float)(f - wide);
+    to = lo <= 0 || !(t + wide <= FLT_MAX) ? INFINITY : (float)(t + wide);
+    if (lo > hi) from = INFINITY, to = -INFINITY;
+  };
+  float kf, kt, pf, pt, df, dt;
+  interval(p.k_bin < 0 ? BINS : p.k_bin, p.k_bin, kf, kt);
+  interval(p.p_lo, p.p_hi, pf, pt);
+  interval(p.d_lo, p.d_hi, df, dt);
   each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
                      min(a.vocab, (b + 1) * chunk), [&](float l, int id) {
-                       if (!s.entry(l)) return;
-                       const double x = s.x_of(l);
-                       if (!p.wants(s.bin_of(x))) return;
-                       bool keep;
-                       s.mass_of(x, keep);
-                       if (!keep) return;
+                       if (!((l >= kf && l <= kt) || (l >= pf && l <= pt) || (l >= df && l <= dt)))
+                         return;
+                       const double y = s.y_of(l);
+                       if (!s.entry(l) || !(y <= s.y_max) || !p.wants(s.bin_of(y))) return;
                        const uint32_t at = atomicAdd(&w.n_cand, 1u);
                        if (at < CAP) w.cand[at] = entry_of(l, id);
                      });
@@ -366,80 +352,60 @@ struct Place {
 };
 
 // First entry, in order, of bin `bin` whose rank (by_mass: cumulative mass) reaches
-// thr, with rank0 and cum0 before the bin: radix search over the row, 11 bits of
-// the entry a pass (the id has at most 20 bits, so the order key's 32 bits and they
-// take 5 passes).
+// thr: radix search over the row, 11 bits of the entry a pass (the id has at most 20
+// bits, so the order key's 32 bits and they take 5 passes).
 template <typename T>
-__device__ Place search(const T* row, int V, const Setting& s, int bin, bool by_mass, u64 thr,
-                        uint32_t rank0, u64 cum0, u64* s_mass, uint32_t* s_cnt) {
-  __shared__ u64 s_m[PICK_T / 64], s_bm;
-  __shared__ uint32_t s_c[PICK_T / 64], s_bc;
-  __shared__ int s_bin;
+__device__ inline Place search(const T* row, int V, const Setting& s, const RowWs& w, int bin,
+                               bool by_mass, u64 thr, u64* s_bin, u64* s_u, int* s_i) {
   constexpr int E = BINS / PICK_T;
-  // the entry's bits from the top: key 31..21, 20..10, 9..0 with the id's complement
-  // above bit 20 fixed, then 20..11 and 10..0 of the complement
-  const int lo[5] = {53, 42, 32, 11, 0}, nb[5] = {11, 11, 10, 10, 11};
-  u64 prefix = 0, fixed = 0;
+  const u64 mass0 = bin ? w.mass[bin - 1] : 0;
+  const uint32_t rank0 = bin ? w.cnt[bin - 1] : 0;
+  const double unit = unit_of(bin);
+  u64 want = thr - rank0;  // in entries, or in units: the fewest whose mass reaches it
+  if (by_mass) {
+    const u64 t = thr - mass0;
+    want = (u64)((double)t / unit);
+    while (mass_of(unit, want) < t) ++want;
+    while (want > 0 && mass_of(unit, want - 1) >= t) --want;
+  }
+  // the entry's bits from the top: key 31..21, 20..10, 9..0, then 20..11 and 10..0 of the
+  // id's complement, whose other bits are ones
+  u64 prefix = 0, fixed = 0, done = 0;  // done: the word of what lies before the digit
   for (int d = 0; d < 5; ++d) {
-    for (int i = threadIdx.x; i < BINS; i += PICK_T) {
-      s_mass[i] = 0;
-      s_cnt[i] = 0;
-    }
+    const int lo = d == 0 ? 53 : d == 1 ? 42 : d == 2 ? 32 : d == 3 ? 11 : 0;
+    const int nb = d == 2 || d == 3 ? 10 : 11;
+    for (int i = threadIdx.x; i < BINS; i += PICK_T) s_bin[i] = 0;
+    if (threadIdx.x == 0) *s_i = BINS - 1;
     __syncthreads();
-    const u64 mask = ((1ull << nb[d]) - 1) << lo[d];
+    const u64 mask = ((1ull << nb) - 1) << lo;
     each_logit<PICK_T>(row, 0, V, [&](float l, int id) {
-      if (!s.entry(l)) return;
-      const double x = s.x_of(l);
-      if (s.bin_of(x) != bin) return;
+      const double y = s.y_of(l);
       const u64 e = entry_of(l, id);
-      if ((e & fixed) != prefix) return;
-      bool keep;
-      const u64 m = s.mass_of(x, keep);
-      if (!keep) return;
+      if (!s.entry(l) || !(y <= s.y_max) || s.bin_of(y) != bin || (e & fixed) != prefix) return;
       // digits in decreasing order
-      const int at = (int)((mask - (e & mask)) >> lo[d]);
-      atomicAdd(&s_cnt[at], 1u);
-      if (m) atomicAdd(&s_mass[at], m);
+      atomicAdd(&s_bin[(mask - (e & mask)) >> lo], (1ull << CNT_AT) + s.s_of(y, bin));
     });
     __syncthreads();
-    u64 hm[E], m = 0;
-    uint32_t hc[E], c = 0;
+    u64 incl[E], x = 0;
+#pragma unroll
+    for (int e = 0; e < E; ++e) incl[e] = x += s_bin[threadIdx.x * E + e];
+    u64 before = block_incl<PICK_T>(x, s_u) - x + done;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      m += s_mass[threadIdx.x * E + e];
-      c += s_cnt[threadIdx.x * E + e];
-      hm[e] = m;
-      hc[e] = c;
-    }
-    const u64 mi = block_incl<PICK_T>(m, s_m) - m + cum0;
-    const uint32_t ci = block_incl<PICK_T>(c, s_c) - c + rank0;
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      hm[e] += mi;
-      hc[e] += ci;
-    }
-    const int at = by_mass ? first_bin<PICK_T>(hm, thr, &s_bm, &s_bin)
-                           : first_bin<PICK_T>(hc, (uint32_t)thr, &s_bc, &s_bin);
-    // rank and mass before the digit, and up to it
-    __syncthreads();
-    if ((int)threadIdx.x == at / E) {
-      u64 x = 0;
-      uint32_t y = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (e == at % E) {
-          x = hm[e];
-          y = hc[e];
-        }
-      s_bm = x - s_mass[at];
-      s_bc = y - s_cnt[at];
+      const u64 up = incl[e] + before;
+      const u64 was = e ? incl[e - 1] + before : before;
+      auto val = [&](u64 v) { return by_mass ? units_of(v) : v >> CNT_AT; };
+      if (val(was) < want && want <= val(up)) {
+        *s_i = threadIdx.x * E + e;
+        s_u[PICK_T / 64] = was;
+      }
     }
     __syncthreads();
-    cum0 = s_bm;
-    rank0 = s_bc;
-    prefix |= mask - ((u64)at << lo[d]);
+    const int at = *s_i;
+    done = s_u[PICK_T / 64];
+    prefix |= mask - ((u64)at << lo);
     fixed |= mask;
-    if (d == 2) {  // ids lie below 2^20: the complement's other bits are ones
+    if (d == 2) {
       const u64 ones = 0xFFFFFFFFull & ~((1ull << 21) - 1);
       prefix |= ones;
       fixed |= ones;
@@ -447,25 +413,44 @@ __device__ Place search(const T* row, int V, const Setting& s, int bin, bool by_
     __syncthreads();
   }
   // one entry is left
-  bool keep;
-  const double x = s.x_of(key_logit((uint32_t)(prefix >> 32)));
-  return Place{prefix, cum0 + s.mass_of(x, keep), rank0 + 1};
+  const double y = s.y_of(key_logit((uint32_t)(prefix >> 32)));
+  const u64 up = done + (1ull << CNT_AT) + s.s_of(y, bin);
+  return Place{prefix, mass0 + mass_of(unit, units_of(up)), rank0 + (uint32_t)(up >> CNT_AT)};
+}
+
+// The three searches, each with what the one before kept.  find(by_mass, thr).
+template <typename F>
+__device__ inline void places(const Plan& p, const Setting& s, F find, u64& ent, u64& z,
+                              uint32_t& kept) {
+  z = p.z;
+  kept = min(s.k, p.total);
+  ent = 0;
+  for (int step = 0; step < 3; ++step) {
+    if (step == 0 ? p.k_bin < 0 : step == 1 && !(s.top_p < 1.0)) continue;
+    const Place q = find(step != 0, step == 0 ? (u64)s.k : step == 1 ? reach(s.top_p, z)
+                                                                     : exceed(s.u, z));
+    if (step < 2) z = q.cum;
+    if (step == 1) kept = q.rank;
+    ent = q.entry;
+  }
 }
 
 // one workgroup a row
 template <typename T>
 __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
-  __shared__ u64 s_e[CAP];  // entries in order; the radix search's masses
-  __shared__ uint32_t s_x[BINS];
-  __shared__ u64 s_gap[BINS];
-  __shared__ u64 s_m[PICK_T / 64];
-  __shared__ uint32_t s_c[PICK_T / 64];
-  __shared__ int s_at;
-  __shared__ u64 s_cum, s_ent;
+  __shared__ u64 s_e[CAP];       // entries in order; the radix search's words
+  __shared__ u64 s_head[BINS];   // units before a bin's first entry
+  __shared__ uint32_t s_first[BINS];
+  __shared__ u64 s_u[PICK_T / 64 + 1], s_cum, s_ent;
   __shared__ uint32_t s_rank;
-  const int r = blockIdx.x;
-  RowWs& w = ((RowWs*)a.ws)[r];
+  __shared__ int s_at;
+  const int r = blockIdx.x, lane = threadIdx.x & 63;
+  const RowWs& w = ((const RowWs*)a.ws)[r];
+  const uint32_t n = w.n_cand;
+  const Plan p = w.plan;
   const Setting s = setting(a, r, row_max(w, NB));
+  u64 ent, z;
+  uint32_t kept;
   if (!s.entry(s.lmax)) {  // every token is barred
     if (threadIdx.x == 0) {
       a.tokens[r] = -1;
@@ -474,15 +459,41 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
     }
     return;
   }
-  Sums<PICK_T> h;
-  const Plan p = plan<PICK_T>(w, s, h);
-  const uint32_t n = w.n_cand;
-  u64 z = p.z;
-  uint32_t kept = min(s.k, p.total);
-  u64 ent = 0;
-  if (n <= CAP) {
+  if (n <= 64) {
+    if (threadIdx.x >= 64) return;
+    const u64 e0 = lane < (int)n ? w.cand[lane] : 0;
+    int rank = 0;
+    for (int i = 0; i < (int)n; ++i) {
+      const u64 x = ((u64)(uint32_t)__builtin_amdgcn_readlane((int)(e0 >> 32), i) << 32) |
+                    (uint32_t)__builtin_amdgcn_readlane((int)e0, i);
+      rank += x > e0;
+    }
+    if (lane < (int)n) s_e[rank] = e0;
+    __builtin_amdgcn_wave_barrier();
+    const u64 e = lane < (int)n ? s_e[lane] : 0;
+    const double y = s.y_of(key_logit((uint32_t)(e >> 32)));
+    const int bin = lane < (int)n ? s.bin_of(y) : -1;
+    const u64 own = bin < 0 ? 0 : (1ull << UNIT) - s.s_of(y, bin);
+    const u64 incl = wave_incl(own);
+    const int prev = __shfl_up(bin, 1);
+    const bool head = lane == 0 || prev != bin;
+    const uint64_t heads = __ballot(head) & (~0ull >> (63 - lane));
+    const int first = 63 - __clzll((long long)heads);
+    const u64 units = incl - __shfl(incl - own, first);
+    u64 cum = 0;
+    uint32_t rk = 0;
+    if (bin >= 0) {
+      cum = (bin ? w.mass[bin - 1] : 0) + mass_of(unit_of(bin), units);
+      rk = (bin ? w.cnt[bin - 1] : 0) + lane - first + 1;
+    }
+    places(p, s, [&](bool by_mass, u64 thr) {
+      const uint64_t hit = __ballot(bin >= 0 && (by_mass ? cum >= thr : (u64)rk >= thr));
+      const int at = hit ? __ffsll((unsigned long long)hit) - 1 : (int)n - 1;
+      return Place{__shfl(e, at), __shfl(cum, at), (uint32_t)__shfl((int)rk, at)};
+    }, ent, z, kept);
+  } else if (n <= CAP) {
     // sort (decreasing), padded with zeros to a power of two
-    int N = 64;
+    int N = 128;
     while (N < (int)n) N <<= 1;
     for (int i = threadIdx.x; i < N; i += PICK_T) s_e[i] = i < (int)n ? w.cand[i] : 0;
     for (int k = 2; k <= N; k <<= 1)
@@ -497,70 +508,53 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
           }
         }
       }
-    // counts and masses of the bins not gathered, up to each bin
-    {
-      constexpr int E = BINS / PICK_T;
-      u64 m = 0, mm[E];
-      uint32_t c = 0, cc[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int b = threadIdx.x * E + e;
-        if (!p.wants(b)) {
-          m += w.mass[b];
-          c += w.cnt[b];
-        }
-        mm[e] = m;
-        cc[e] = c;
-      }
-      const u64 mi = block_incl<PICK_T>(m, s_m) - m;
-      const uint32_t ci = block_incl<PICK_T>(c, s_c) - c;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        s_gap[threadIdx.x * E + e] = mm[e] + mi;
-        s_x[threadIdx.x * E + e] = cc[e] + ci;
-      }
-    }
     __syncthreads();
     // rank and cumulative mass of each entry, CAP / PICK_T a thread
     constexpr int E = CAP / PICK_T;
     u64 cum[E], m = 0;
     uint32_t rank[E];
+    int bin[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int i = threadIdx.x * E + e;
+      bin[e] = -1;
       if (i < (int)n) {
-        bool keep;
-        m += s.mass_of(s.x_of(key_logit((uint32_t)(s_e[i] >> 32))), keep);
+        const double y = s.y_of(key_logit((uint32_t)(s_e[i] >> 32)));
+        bin[e] = s.bin_of(y);
+        m += (1ull << UNIT) - s.s_of(y, bin[e]);
       }
       cum[e] = m;
     }
-    const u64 mi = block_incl<PICK_T>(m, s_m) - m;
+    const u64 m0 = block_incl<PICK_T>(m, s_u) - m;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int i = threadIdx.x * E + e;
-      cum[e] += mi;
-      rank[e] = i + 1;
-      if (i < (int)n) {
-        const int b = s.bin_of(s.x_of(key_logit((uint32_t)(s_e[i] >> 32))));
-        cum[e] += s_gap[b];
-        rank[e] += s_x[b];
+      if (bin[e] < 0) continue;
+      const int prev = i ? s.bin_of(s.y_of(key_logit((uint32_t)(s_e[i - 1] >> 32)))) : -1;
+      if (prev != bin[e]) {
+        s_head[bin[e]] = m0 + (e ? cum[e - 1] : 0);
+        s_first[bin[e]] = i;
       }
     }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int b = bin[e];
+      if (b < 0) continue;
+      cum[e] = (b ? w.mass[b - 1] : 0) + mass_of(unit_of(b), cum[e] + m0 - s_head[b]);
+      rank[e] = (b ? w.cnt[b - 1] : 0) + threadIdx.x * E + e - s_first[b] + 1;
+    }
     // first entry that reaches a rank or a mass
-    auto find = [&](bool by_mass, u64 thr) {
-      __syncthreads();
-      if (threadIdx.x == 0) s_at = INT32_MAX;
+    places(p, s, [&](bool by_mass, u64 thr) {
+      if (threadIdx.x == 0) s_at = (int)n - 1;
       __syncthreads();
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int i = threadIdx.x * E + e;
-        if (i < (int)n && (by_mass ? cum[e] >= thr : rank[e] >= (uint32_t)thr)) {
-          atomicMin(&s_at, i);
-          break;
-        }
-      }
+      for (int e = E - 1; e >= 0; --e)
+        if (bin[e] >= 0 && (by_mass ? cum[e] >= thr : (u64)rank[e] >= thr) &&
+            !(e > 0 && (by_mass ? cum[e - 1] >= thr : (u64)rank[e - 1] >= thr)))
+          atomicMin(&s_at, (int)threadIdx.x * E + e);
       __syncthreads();
-      const int at = min(s_at, (int)n - 1);
+      const int at = s_at;
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if ((int)threadIdx.x * E + e == at) {
@@ -570,46 +564,28 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
         }
       __syncthreads();
       return Place{s_ent, s_cum, s_rank};
-    };
-    if (p.k_bin >= 0) z = find(false, s.k).cum;
-    if (s.top_p < 1.0) {
-      const Place q = find(true, reach(s.top_p, z));
-      z = q.cum;
-      kept = q.rank;
-    }
-    ent = find(true, exceed(s.u, z)).entry;
+    }, ent, z, kept);
   } else {
     const T* row = (const T*)a.logits + (size_t)r * a.ld;
-    __shared__ u64 s_bm;
-    __shared__ uint32_t s_bc;
-    __shared__ int s_bin;
-    constexpr int E = BINS / PICK_T;
-    auto find = [&](bool by_mass, u64 thr) {
-      const int b = by_mass ? first_bin<PICK_T>(h.m, thr, &s_bm, &s_bin)
-                            : first_bin<PICK_T>(h.c, (uint32_t)thr, &s_bc, &s_bin);
-      __syncthreads();
-      if ((int)threadIdx.x == b / E) {
+    places(p, s, [&](bool by_mass, u64 thr) {
+      // the place's bin
+      constexpr int E = BINS / PICK_T;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (e == b % E) {
-            s_bm = h.m[e] - w.mass[b];
-            s_bc = h.c[e] - w.cnt[b];
-          }
+      for (int e = 0; e < E; ++e) {
+        const int b = threadIdx.x * E + e;
+        const u64 up = by_mass ? w.mass[b] : w.cnt[b];
+        const u64 was = !b ? 0 : by_mass ? w.mass[b - 1] : w.cnt[b - 1];
+        if (was < thr && thr <= up) s_at = b;
       }
       __syncthreads();
-      return search<T>(row, a.vocab, s, b, by_mass, thr, s_bc, s_bm, s_e, s_x);
-    };
-    if (p.k_bin >= 0) z = find(false, s.k).cum;
-    if (s.top_p < 1.0) {
-      const Place q = find(true, reach(s.top_p, z));
-      z = q.cum;
-      kept = q.rank;
-    }
-    ent = find(true, exceed(s.u, z)).entry;
+      const int b = s_at;
+      __syncthreads();
+      return search<T>(row, a.vocab, s, w, b, by_mass, thr, s_e, s_u, &s_at);
+    }, ent, z, kept);
   }
   if (threadIdx.x == 0) {
     a.tokens[r] = (int32_t)~(uint32_t)ent;
-    const double x = s.x_of(key_logit((uint32_t)(ent >> 32)));
+    const double x = s.y_of(key_logit((uint32_t)(ent >> 32))) * (-1.0 / BIN_W);
     if (a.logprob) a.logprob[r] = (float)(x - log((double)z * (1.0 / (double)(1ull << FRAC))));
     if (a.kept) a.kept[r] = (int32_t)kept;
   }

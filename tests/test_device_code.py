@@ -65,7 +65,7 @@ def test_split_sums_take_rows_at_any_float_address(tmp_path):
         assert ("4" in loads) == resid, loads
 
 
-@pytest.mark.parametrize("src", ["paged.hip"])
+@pytest.mark.parametrize("src", ["paged.hip", "draw.hip"])
 def test_no_scalar_register_spills(src, tmp_path):
     """Scalar registers spilled to lanes of a vector register at the head of a block
     make the compiler place copies of vector registers there before the block restores
