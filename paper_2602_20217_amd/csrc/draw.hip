@@ -25,7 +25,10 @@
 //                 wave, up to CAP in a sort; a row whose bins hold more (equal logits,
 //                 high temperature) finds each place digit by digit over the whole row
 //
-// 256 rows of 128256 logits (131 MB): @256@
+// 256 rows of 128256 logits (131 MB): 20 + 26 + 33 + 13 us, three readings
+// at 3.9 to 6.7 TB/s that share the time with the bins' arithmetic, and the ordering of
+// the densest row.  One such row: 3 + 5 + 7 + 4, the latency of four launches and their
+// barriers.
 #include "ks_internal.h"
 
 #include <algorithm>
@@ -89,16 +92,22 @@ __device__ inline u64 entry_of(float l, int id) {
   return ((u64)order_key(l) << 32) | (uint32_t)~id;
 }
 
-// f(logit, id) for the ids [n0, n1) of a row, by NT threads.
+// f(logit, id) for the ids [n0, n1) of a row, by NT threads; the next load is under
+// way while one's logits are dealt with.  (Four at a time: 256 rows of 128256 22 us in
+// k_draw_max for 20, 40 in k_draw_gather for 33, and 27 in k_draw_hist for 29.)
 template <int NT, typename T, typename F>
 __device__ inline void each_logit(const T* row, int n0, int n1, F f) {
   constexpr int E = 16 / sizeof(T);
   if (((uintptr_t)(row + n0) & 15) == 0) {
     const int nv = (n1 - n0) / E;
-#pragma unroll 4
+    const uint4* v = (const uint4*)(row + n0);
+    uint4 q, next;
+    if ((int)threadIdx.x < nv) next = v[threadIdx.x];
     for (int i = threadIdx.x; i < nv; i += NT) {
+      q = next;
+      if (i + NT < nv) next = v[i + NT];
       T x[E];
-      *(uint4*)x = *(const uint4*)(row + n0 + E * i);
+      *(uint4*)x = q;
 #pragma unroll
       for (int e = 0; e < E; ++e) f(ld_logit(&x[e]), n0 + E * i + e);
     }
@@ -115,17 +124,32 @@ struct Setting {
   uint32_t k;
   float lmax;
   __device__ static bool entry(float l) { return l > -INFINITY; }  // not barred, not NaN
-  // place of an entry in bins, from the largest down
+  // 64 (largest - logit) / temperature
   __device__ double y_of(float l) const {
     return l == lmax ? 0.0 : ((double)lmax - (double)l) * scale;
   }
-  __device__ static int bin_of(double y) { return y < BINS - 1 ? (int)y : BINS - 1; }
-  // s of an entry: 1 - e^-r = r (1 - r/2 (1 - r/3 (1 - r/4))) to 2^-31
-  __device__ static uint32_t s_of(double y, int bin) {
-    if (bin == BINS - 1) return 0;
-    const float r = (float)(y - bin) * (float)(1.0 / BIN_W);
-    const float t = r * fmaf(r * -0.5f, fmaf(r * (-1.0f / 3), fmaf(r, -0.25f, 1.0f), 1.0f), 1.0f);
-    return (uint32_t)(t * 2147483648.0f + 0.5f);
+  // Bin of an entry and its remainder in units of 2^-31 of a bin, the last bin's 0; false
+  // for what is no entry or falls to min-p.  Added to 2^21, a place has its bin and
+  // remainder as the low bits of the sum.  (inf - inf is 0 here.)
+  __device__ bool place(float l, int& bin, uint32_t& rem) const {
+    const double y = ((double)lmax - (double)l) * scale;
+    if (!entry(l) || y > y_max) return false;
+    const double t = fmin(fmax(y, 0.0), (double)(BINS - 1)) + (double)(1 << (52 - UNIT));
+    const u64 u = __double_as_longlong(t);
+    bin = (int)(u >> UNIT) & (BINS - 1);
+    rem = (uint32_t)u & ((1u << UNIT) - 1);
+    return true;
+  }
+  __device__ int bin_of(float l) const {
+    int b;
+    uint32_t rem;
+    return place(l, b, rem) ? b : BINS - 1;
+  }
+  // s of a remainder: 1 - e^-r = r (1 - r/2 (1 - r/3 (1 - r/4))) to 2^-31
+  __device__ static uint32_t s_of(uint32_t rem) {
+    const float x = (float)rem * (float)(1.0 / BIN_W);
+    const float r = x * (1.0f / (1u << UNIT));
+    return (uint32_t)fmaf(x, fmaf(r * -0.5f, fmaf(r * (-1.0f / 3), fmaf(r, -0.25f, 1.0f), 1.0f), 1.0f), 0.5f);
   }
 };
 __device__ inline Setting setting(const DrawArgs& a, int r, float lmax) {
@@ -144,9 +168,11 @@ __device__ inline Setting setting(const DrawArgs& a, int r, float lmax) {
   s.lmax = lmax;
   return s;
 }
-// units of mass that one unit of 1 - s has in a bin
+// units of mass that one unit of 1 - s has in a bin: e^-8i/64 e^-j/64, whose second
+// factors are constants where a thread has bins in a row
 __device__ inline double unit_of(int bin) {
-  return bin == BINS - 1 ? 0.0 : exp(-bin / BIN_W) * (double)(1ull << (FRAC - UNIT));
+  constexpr double W[8] = {1.0, 0.98449643700540845, 0.96923323447634413, 0.95420666596918835, 0.93941306281347581, 0.92484881321620482, 0.91051036138003416, 0.89639420663515046};
+  return bin == BINS - 1 ? 0.0 : exp((bin >> 3) * (-8 / BIN_W)) * W[bin & 7] * (double)(1ull << (FRAC - UNIT));
 }
 // units of 1 - s of a bin's word, and their mass
 __device__ inline u64 units_of(u64 w) {
@@ -179,17 +205,15 @@ __device__ inline V block_incl(V v, V* sh) {
   return v;
 }
 
-// Bins in which an inclusive sum first reaches a threshold; E bins a thread.
-// incl: the thread's inclusive sums, before: the sum before its first.
+// The bin, if a thread has it, in which an inclusive sum first reaches a threshold; E bins
+// a thread.  incl: the thread's inclusive sums, before: the sum before its first.
 template <int E, typename V>
-__device__ inline int own_bin(const V (&incl)[E], V before, V thr) {
-  int at = -1;
+__device__ inline void own_bin(const V (&incl)[E], V before, V thr, int& at) {
+  if (before >= thr || thr > incl[E - 1]) return;
+  int n = 0;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if (at < 0 && before < thr && thr <= incl[e]) at = threadIdx.x * E + e;
-    before = incl[e];
-  }
-  return at;
+  for (int e = 0; e < E - 1; ++e) n += incl[e] < thr;
+  at = threadIdx.x * E + n;
 }
 
 // The plan of a row, with the inclusive sums of its bins in mass and cnt (LDS).
@@ -199,14 +223,14 @@ __device__ inline Plan plan(const RowWs& w, const Setting& s, u64* mass, uint32_
   __shared__ u64 s_m[NT / 64];
   __shared__ uint32_t s_c[NT / 64];
   __shared__ int s_bin[2];
-  u64 m = 0, hm[E];
+  u64 m = 0, hm[E], x[E];
   uint32_t c = 0, hc[E];
 #pragma unroll
+  for (int e = 0; e < E; ++e) x[e] = w.bin[threadIdx.x * E + e];
+#pragma unroll
   for (int e = 0; e < E; ++e) {
-    const int b = threadIdx.x * E + e;
-    const u64 x = w.bin[b];
-    if (x) m += mass_of(unit_of(b), units_of(x));
-    c += (uint32_t)(x >> CNT_AT);
+    m += mass_of(unit_of(threadIdx.x * E + e), units_of(x[e]));
+    c += (uint32_t)(x[e] >> CNT_AT);
     hm[e] = m;
     hc[e] = c;
   }
@@ -223,10 +247,13 @@ __device__ inline Plan plan(const RowWs& w, const Setting& s, u64* mass, uint32_
   p.z = mass[BINS - 1];
   // the bins of up to two thresholds
   auto find2 = [&](bool by_mass, u64 a, u64 b, int& ba, int& bb) {
-    const int x = by_mass ? own_bin<E>(hm, m0, a) : own_bin<E>(hc, c0, (uint32_t)a);
-    const int y = by_mass ? own_bin<E>(hm, m0, b) : own_bin<E>(hc, c0, (uint32_t)b);
-    if (x >= 0) s_bin[0] = x;
-    if (y >= 0) s_bin[1] = y;
+    if (by_mass) {
+      own_bin<E>(hm, m0, a, s_bin[0]);
+      own_bin<E>(hm, m0, b, s_bin[1]);
+    } else {
+      own_bin<E>(hc, c0, (uint32_t)a, s_bin[0]);
+      own_bin<E>(hc, c0, (uint32_t)b, s_bin[1]);
+    }
     __syncthreads();
     ba = s_bin[0];
     bb = s_bin[1];
@@ -295,10 +322,10 @@ __global__ __launch_bounds__(SCAN_T) void k_draw_hist(DrawArgs a, int chunk) {
   __syncthreads();
   each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
                      min(a.vocab, (b + 1) * chunk), [&](float l, int) {
-                       const double y = s.y_of(l);
-                       if (!s.entry(l) || !(y <= s.y_max)) return;
-                       const int bin = s.bin_of(y);
-                       atomicAdd(&s_bin[bin], (1ull << CNT_AT) + s.s_of(y, bin));
+                       int bin;
+                       uint32_t rem;
+                       if (s.place(l, bin, rem))
+                         atomicAdd(&s_bin[bin], (1ull << CNT_AT) + s.s_of(rem));
                      });
   __syncthreads();
   for (int i = threadIdx.x; i < BINS; i += SCAN_T)
@@ -307,8 +334,11 @@ __global__ __launch_bounds__(SCAN_T) void k_draw_hist(DrawArgs a, int chunk) {
 
 template <typename T>
 __global__ __launch_bounds__(SCAN_T) void k_draw_gather(DrawArgs a, int chunk) {
-  __shared__ u64 s_mass[BINS];
-  __shared__ uint32_t s_cnt[BINS];
+  __shared__ u64 s_e[CAP];  // the bins' sums, then entries
+  __shared__ uint32_t s_n;
+  static_assert(CAP * sizeof(u64) >= BINS * (sizeof(u64) + sizeof(uint32_t)));
+  u64* const s_mass = s_e;
+  uint32_t* const s_cnt = (uint32_t*)(s_e + BINS);
   const int b = blockIdx.x, r = blockIdx.y;
   RowWs& w = ((RowWs*)a.ws)[r];
   const Setting s = setting(a, r, row_max(w, gridDim.x));
@@ -321,11 +351,14 @@ __global__ __launch_bounds__(SCAN_T) void k_draw_gather(DrawArgs a, int chunk) {
     }
     if (threadIdx.x == 0) w.plan = p;
   }
+  if (threadIdx.x == 0) s_n = 0;
+  __syncthreads();  // the sums' place takes entries from here on
   // logits that may lie in the bins lo .. hi: a float32 interval, wider by more than
   // its roundings
+  const double w_bin = 1.0 / s.scale;
   auto interval = [&](int lo, int hi, float& from, float& to) {
-    const double f = (double)s.lmax - (hi + 1) / s.scale, t = (double)s.lmax - lo / s.scale;
-    const double wide = 1e-6 * (fabs((double)s.lmax) + (hi + 1) / s.scale) + 1e-30;
+    const double f = (double)s.lmax - (hi + 1) * w_bin, t = (double)s.lmax - lo * w_bin;
+    const double wide = 1e-6 * (fabs((double)s.lmax) + (hi + 1) * w_bin) + 1e-30;
     from = hi >= BINS - 1 || !(f - wide >= -FLT_MAX) ? -INFINITY : (float)(f - wide);
     to = lo <= 0 || !(t + wide <= FLT_MAX) ? INFINITY : (float)(t + wide);
     if (lo > hi) from = INFINITY, to = -INFINITY;
@@ -334,15 +367,31 @@ __global__ __launch_bounds__(SCAN_T) void k_draw_gather(DrawArgs a, int chunk) {
   interval(p.k_bin < 0 ? BINS : p.k_bin, p.k_bin, kf, kt);
   interval(p.p_lo, p.p_hi, pf, pt);
   interval(p.d_lo, p.d_hi, df, dt);
+  const float lo = fminf(kf, fminf(pf, df)), hi = fmaxf(kt, fmaxf(pt, dt));
+  // Entries of the intervals first, by float32 alone, then the bins' own of these.  (The
+  // exact test at each logit's place in the loop makes its code several times as long.)  More than CAP count as more than CAP in the bins.
   each_logit<SCAN_T>((const T*)a.logits + (size_t)r * a.ld, b * chunk,
                      min(a.vocab, (b + 1) * chunk), [&](float l, int id) {
+                       if (!(l >= lo && l <= hi)) return;
                        if (!((l >= kf && l <= kt) || (l >= pf && l <= pt) || (l >= df && l <= dt)))
                          return;
-                       const double y = s.y_of(l);
-                       if (!s.entry(l) || !(y <= s.y_max) || !p.wants(s.bin_of(y))) return;
-                       const uint32_t at = atomicAdd(&w.n_cand, 1u);
-                       if (at < CAP) w.cand[at] = entry_of(l, id);
+                       const uint32_t n = atomicAdd(&s_n, 1u);
+                       if (n < CAP) s_e[n] = entry_of(l, id);
                      });
+  __syncthreads();
+  const uint32_t n = s_n;
+  if (n > CAP) {
+    if (threadIdx.x == 0) atomicAdd(&w.n_cand, CAP + 1u);
+    return;
+  }
+  for (uint32_t i = threadIdx.x; i < n; i += SCAN_T) {
+    const u64 e = s_e[i];
+    int bin;
+    uint32_t rem;
+    if (!s.place(key_logit((uint32_t)(e >> 32)), bin, rem) || !p.wants(bin)) continue;
+    const uint32_t at = atomicAdd(&w.n_cand, 1u);
+    if (at < CAP) w.cand[at] = e;
+  }
 }
 
 // The place searched for: the entry, and rank and cumulative mass up to it.
@@ -379,11 +428,12 @@ __device__ inline Place search(const T* row, int V, const Setting& s, const RowW
     __syncthreads();
     const u64 mask = ((1ull << nb) - 1) << lo;
     each_logit<PICK_T>(row, 0, V, [&](float l, int id) {
-      const double y = s.y_of(l);
+      int b;
+      uint32_t rem;
       const u64 e = entry_of(l, id);
-      if (!s.entry(l) || !(y <= s.y_max) || s.bin_of(y) != bin || (e & fixed) != prefix) return;
+      if (!s.place(l, b, rem) || b != bin || (e & fixed) != prefix) return;
       // digits in decreasing order
-      atomicAdd(&s_bin[(mask - (e & mask)) >> lo], (1ull << CNT_AT) + s.s_of(y, bin));
+      atomicAdd(&s_bin[(mask - (e & mask)) >> lo], (1ull << CNT_AT) + s.s_of(rem));
     });
     __syncthreads();
     u64 incl[E], x = 0;
@@ -413,8 +463,10 @@ __device__ inline Place search(const T* row, int V, const Setting& s, const RowW
     __syncthreads();
   }
   // one entry is left
-  const double y = s.y_of(key_logit((uint32_t)(prefix >> 32)));
-  const u64 up = done + (1ull << CNT_AT) + s.s_of(y, bin);
+  int b;
+  uint32_t rem = 0;
+  s.place(key_logit((uint32_t)(prefix >> 32)), b, rem);
+  const u64 up = done + (1ull << CNT_AT) + s.s_of(rem);
   return Place{prefix, mass0 + mass_of(unit, units_of(up)), rank0 + (uint32_t)(up >> CNT_AT)};
 }
 
@@ -471,9 +523,10 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
     if (lane < (int)n) s_e[rank] = e0;
     __builtin_amdgcn_wave_barrier();
     const u64 e = lane < (int)n ? s_e[lane] : 0;
-    const double y = s.y_of(key_logit((uint32_t)(e >> 32)));
-    const int bin = lane < (int)n ? s.bin_of(y) : -1;
-    const u64 own = bin < 0 ? 0 : (1ull << UNIT) - s.s_of(y, bin);
+    int bin = -1;
+    uint32_t rem = 0;
+    if (lane < (int)n) s.place(key_logit((uint32_t)(e >> 32)), bin, rem);
+    const u64 own = bin < 0 ? 0 : (1ull << UNIT) - s.s_of(rem);
     const u64 incl = wave_incl(own);
     const int prev = __shfl_up(bin, 1);
     const bool head = lane == 0 || prev != bin;
@@ -492,11 +545,24 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
       return Place{__shfl(e, at), __shfl(cum, at), (uint32_t)__shfl((int)rk, at)};
     }, ent, z, kept);
   } else if (n <= CAP) {
-    // sort (decreasing), padded with zeros to a power of two
+    // into decreasing order: up to one a thread by counting the larger ones, N a power of
+    // two of places and PICK_T / N threads a place; more by a bitonic sort, padded with
+    // zeros.  (The sort alone: 256 rows of 128256 16 us for 13.)
     int N = 128;
     while (N < (int)n) N <<= 1;
     for (int i = threadIdx.x; i < N; i += PICK_T) s_e[i] = i < (int)n ? w.cand[i] : 0;
-    for (int k = 2; k <= N; k <<= 1)
+    if (N <= PICK_T) {
+      const int at = threadIdx.x & (N - 1), part = threadIdx.x / N;
+      const int per = ((int)n + PICK_T / N - 1) / (PICK_T / N);
+      s_first[threadIdx.x] = 0;
+      __syncthreads();
+      const u64 x = s_e[at];
+      uint32_t larger = 0;
+      for (int i = part * per; i < min((int)n, (part + 1) * per); ++i) larger += s_e[i] > x;
+      if (at < (int)n) atomicAdd(&s_first[at], larger);
+      __syncthreads();
+      if (part == 0 && at < (int)n) s_e[s_first[at]] = x;
+    } else for (int k = 2; k <= N; k <<= 1)
       for (int j = k >> 1; j > 0; j >>= 1) {
         __syncthreads();
         for (int i = threadIdx.x; i < N / 2; i += PICK_T) {
@@ -519,9 +585,9 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
       const int i = threadIdx.x * E + e;
       bin[e] = -1;
       if (i < (int)n) {
-        const double y = s.y_of(key_logit((uint32_t)(s_e[i] >> 32)));
-        bin[e] = s.bin_of(y);
-        m += (1ull << UNIT) - s.s_of(y, bin[e]);
+        uint32_t rem = 0;
+        s.place(key_logit((uint32_t)(s_e[i] >> 32)), bin[e], rem);
+        m += (1ull << UNIT) - s.s_of(rem);
       }
       cum[e] = m;
     }
@@ -530,7 +596,7 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
     for (int e = 0; e < E; ++e) {
       const int i = threadIdx.x * E + e;
       if (bin[e] < 0) continue;
-      const int prev = i ? s.bin_of(s.y_of(key_logit((uint32_t)(s_e[i - 1] >> 32)))) : -1;
+      const int prev = i ? s.bin_of(key_logit((uint32_t)(s_e[i - 1] >> 32))) : -1;
       if (prev != bin[e]) {
         s_head[bin[e]] = m0 + (e ? cum[e - 1] : 0);
         s_first[bin[e]] = i;
@@ -596,8 +662,11 @@ __global__ __launch_bounds__(PICK_T) void k_draw_pick(DrawArgs a, int NB) {
 size_t draw_ws_bytes(int rows) { return (size_t)rows * sizeof(RowWs); }
 
 void draw_rows(const DrawArgs& a, hipStream_t st) {
-  // chunks: about 1024 workgroups over the rows, of at least 1024 logits
-  int NB = std::min(std::min(NB_MAX, (1024 + a.rows - 1) / a.rows), (a.vocab + 1023) / 1024);
+  // chunks: about 1024 workgroups over the rows, of at least 2560 logits: more chunks add
+  // more bins to memory (7 rows of 151936 in chunks of 1220: k_draw_hist 11.5 us, of 2560
+  // 6.9), fewer leave the chip empty (one row of 128256 in chunks of 4096: 5.9 for 4.8);
+  // 512 workgroups for 256 rows: 48 us for 40 in k_draw_gather, 2048 the same
+  int NB = std::min(std::min(NB_MAX, (1024 + a.rows - 1) / a.rows), (a.vocab + 2560 - 1) / 2560);
   const int chunk = ((a.vocab + NB - 1) / NB + 7) / 8 * 8;
   NB = (a.vocab + chunk - 1) / chunk;
   const dim3 grid(NB, a.rows);
