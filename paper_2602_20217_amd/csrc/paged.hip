@@ -481,8 +481,8 @@ constexpr int KT = 64;          // keys of a tile
 // the 16 consecutive keys from 16 g: one granule of values.
 //  keys    as they lie in memory: register u, lane l has bytes 1024 u + 16 l of the
 //          tile's rows.  (Loaded as operands instead, every lane of a quad another
-//          row, the loads took four times the cache accesses and held the kernel
-//          at 4.4 TB/s whatever the occupancy.)
+//          row, the loads take four times the cache accesses; 64 sequences of 500 to
+//          15000 tokens took 249 us for 238.)
 //  values  lane (i, g): dim 16 db + i, tokens 16 g..16 g + 15
 template <int HD, bool E4>
 struct Tile {
@@ -575,7 +575,8 @@ constexpr int dec_wgs(int HD, bool E4, int QP, int CB) {
 // query head c % G of the kv head); wave w takes the split's tiles w, w + 4, ...
 // and runs a softmax with a running maximum and sum over them.  The next keys are
 // requested when these have gone to LDS and the next values when these are added,
-// so a tile's loads are in flight during the arithmetic of the one before.  The four results meet in LDS, in wave order.
+// so a tile's loads are in flight during the arithmetic of the one before.  The four
+// results meet in LDS, in wave order.
 //
 // A column's arithmetic depends on its own query and length and on the split
 // only, never on the other columns or on CB.
@@ -1072,6 +1073,10 @@ __device__ inline void column(const PagedAttn& a, const SeqRows& sr, int b,
 //                 r in which the 8 lanes of a read differ; those of a write have
 //                 every second chunk)
 //  values in LDS  [granule][half of 8 tokens][dim], 16 bytes
+// The matrix units bound it, with the vector arithmetic of the softmax between their
+// products: 2048 rows of 32 heads, 235 GFLOP, in 306 us (770 TFLOP/s; a library product
+// of 8192 cubed 1239).  128 columns a workgroup and two of them a CU: one works on its
+// scores while the other multiplies; 64 columns with 16x16x32 products took 560 us.
 // Masked places as in k_pg_dec; where an infinite or NaN value lies between the
 // shortest and the longest length of a wave's columns they are computed again, one at
 // a time (`column`).
@@ -1469,7 +1474,10 @@ void paged_append(const PagedAppend& a_, hipStream_t st) {
 }
 
 // Which kernel: a sequence of up to DEC_COLS query columns (rows times query heads of
-// a kv head) goes to the split kernel, one of more to the chunk kernel.
+// a kv head) goes to the split kernel, which reads the cache once per 32 of them, one of
+// more to the chunk kernel, once per 128.  Split and chunk kernel, e4m3, 8 kv heads: 64
+// columns over 8192 tokens 19 and 24 us, over 32768 34 and 39, 16 sequences over 4096 52
+// and 59; 96 columns 32 and 23, 78 and 40, 99 and 59.
 constexpr int DEC_COLS = 64;
 
 PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int planes) {
@@ -1481,12 +1489,14 @@ PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int plane
   // rest being their start and the merge), none shorter than a tile for every wave,
   // and none longer than 4096 positions, which keeps sequences of different lengths
   // level (64 of 500 to 15000 tokens: 216 us, 225 to 250 with one split each).
-  // Of the chunk kernel: what fills the CUs, none shorter than 8 tiles.
-  const int width = chunk ? (128) : 32;
+  // Of the chunk kernel: as many as give every CU two workgroups, none shorter than 4
+  // tiles (256 rows of 4 heads a kv head, one sequence of 32768: 167 us, 215 with one
+  // workgroup a CU, 182 with four; 32 rows over 2048 tokens: 17 us, 22 with 8 tiles).
+  const int width = chunk ? 128 : 32;
   const int blocks = B * hkv * ((cols + width - 1) / width);
-  const int least = chunk ? 8 * KT : DEC_NW * KT;
+  const int least = chunk ? 4 * KT : DEC_NW * KT;
   const int most = std::max(1, (max_len + least - 1) / least);
-  int want = chunk ? 256 / std::max(1, std::min(blocks, 256)) : (255 + blocks) / blocks;
+  int want = chunk ? 512 / std::max(1, std::min(blocks, 512)) : (255 + blocks) / blocks;
   if (!chunk || B > 1) want = std::max(want, (max_len + 4095) / 4096);
   p.chunk = chunk;
   p.nsplit = std::max(1, std::min(want, most));
