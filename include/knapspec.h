@@ -557,9 +557,11 @@ ks_status ks_paged_append(const ks_paged_cache* cache, const ks_paged_rows* rows
  * lse -inf.  Values
  * and keys past a row's position do not reach it, whatever they hold.  lse: float32
  * [rows][hq] or NULL, log of the sum of exp(scale q.k).  scale must be finite.
- * workspace: ks_paged_attention_workspace_bytes() bytes; nothing in it needs to
- * start at any value, and calls (or captured graphs) that may run at the same time
- * need one each.  Asynchronous on stream.
+ * workspace: ks_paged_attention_workspace_bytes() bytes, which are enough for every
+ * call with at most these B, rows, max_rows and max_len (clipped to what the table
+ * holds) and the same hq and cache.  Nothing in it needs to start at any value; calls
+ * (or captured graphs) that may run at the same time need one each.  Asynchronous on
+ * stream.
  */
 size_t ks_paged_attention_workspace_bytes(const ks_paged_cache* cache, int B, int rows, int hq,
                                           int max_rows, int max_len);

@@ -164,7 +164,7 @@ __device__ inline Setting setting(const DrawArgs& a, int r, float lmax) {
   s.k = k > 0 ? (uint32_t)k : 0xFFFFFFFFu;
   s.y_max = mp > 0.f ? -BIN_W * log(fmin((double)mp, 1.0)) : (double)INFINITY;
   s.top_p = tp < 1.f ? fmax((double)tp, 0.0) : 1.0;
-  s.u = u > 0.f ? (double)u : 0.0;
+  s.u = u > 0.f ? fmin((double)u, 1.0) : 0.0;
   s.lmax = lmax;
   return s;
 }

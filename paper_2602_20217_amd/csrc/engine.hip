@@ -925,10 +925,11 @@ ks_status ks_use_paged(ks_ctx* c, const ks_paged_cache* layers, const int32_t* t
         return KS_ECAPACITY;
       }
     }
-    std::vector<int32_t> host(table_len);
-    HIPCHK(hipMemcpyAsync(host.data(), table, (size_t)table_len * 4, hipMemcpyDeviceToHost, c->st));
+    const int used = (c->md.n_max + least - 1) / least;
+    std::vector<int32_t> host(used);
+    HIPCHK(hipMemcpyAsync(host.data(), table, (size_t)used * 4, hipMemcpyDeviceToHost, c->st));
     HIPCHK(hipStreamSynchronize(c->st));
-    for (int i = 0; i < (c->md.n_max + least - 1) / least; ++i)
+    for (int i = 0; i < used; ++i)
       REQ(host[i] >= 0 && host[i] < fewest, "a page of the table is out of range");
   }
   c->pages = pages;
@@ -1241,11 +1242,9 @@ size_t ks_paged_attention_workspace_bytes(const ks_paged_cache* cache, int B, in
       hq < cache->hkv || hq % cache->hkv || max_rows < 1 || max_len < 1)
     return 0;
   if (B == 0 || rows == 0) return 256;
-  int ns = 1;  // of either dtype
-  for (int planes : {1, 3})
-    ns = std::max(ns, ks::paged_plan(B, cache->hkv, hq / cache->hkv, std::min(max_rows, rows),
-                                     max_len, planes).nsplit);
-  return ns > 1 ? (size_t)rows * hq * ns * (cache->hd + 2) * 4 : 256;
+  const long long n =
+      ks::paged_split_rows(hq, hq / cache->hkv, rows, std::min(max_rows, rows), max_len);
+  return std::max<size_t>((size_t)n * hq * (cache->hd + 2) * 4, 256);
 }
 
 ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* rows,
@@ -1268,7 +1267,7 @@ ks_status ks_paged_attention(const ks_paged_cache* cache, const ks_paged_rows* r
   const int G = hq / cache->hkv;
   const int len = std::max(1, rows->max_len);
   const ks::PagedPlan plan =
-      ks::paged_plan(rows->B, cache->hkv, G, a.rows.max_rows, len, dtype == KS_BF16 ? 1 : 3);
+      ks::paged_plan(rows->B, cache->hkv, G, rows->rows, a.rows.max_rows, len);
   const int ns = plan.nsplit;
   REQ((long long)ns * cache->hkv * ((long long)a.rows.max_rows * G / 16 + 1) * rows->B < (1ll << 31) &&
           (long long)rows->rows * hq < (1ll << 31),

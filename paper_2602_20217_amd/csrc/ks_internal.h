@@ -276,10 +276,10 @@ struct PagedAttn {
 void paged_attention(const PagedAttn& a, hipStream_t st);
 // Splits of a call over at most max_rows rows a sequence and max_len positions.
 struct PagedPlan {
-  bool chunk;  // the longest sequences go to the chunk kernel
   int nsplit, span;
 };
-PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int planes);
+PagedPlan paged_plan(int B, int hkv, int G, int rows, int max_rows, int max_len);
+long long paged_split_rows(int hq, int G, int rows, int max_rows, int max_len);
 
 // ---------------------------------------------------- vocabulary reductions
 // argmax (lowest index on ties) and top-1 probability of each of M rows of V

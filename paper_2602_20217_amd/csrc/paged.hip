@@ -1480,8 +1480,16 @@ void paged_append(const PagedAppend& a_, hipStream_t st) {
 // and 59; 96 columns 32 and 23, 78 and 40, 99 and 59.
 constexpr int DEC_COLS = 64;
 
-PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int planes) {
-  PagedPlan p{};
+constexpr int SPAN_MAX = 4096;
+constexpr int SPAN_MIN = 4 * KT;
+// rows times splits that a call with few blocks may add to its rows (see paged_plan):
+// 255 workgroups of 32 columns, or 512 of 128
+static int split_room(int hq, int cols) {
+  return ((cols > DEC_COLS ? 512 * 128 : 255 * 32) + hq - 1) / hq;
+}
+
+PagedPlan paged_plan(int B, int hkv, int G, int rows, int max_rows, int max_len) {
+  PagedPlan p;
   const int cols = max_rows * G;
   const bool chunk = cols > DEC_COLS;
   // Splits of the split kernel: as many as give every CU a workgroup (one sequence of
@@ -1494,14 +1502,23 @@ PagedPlan paged_plan(int B, int hkv, int G, int max_rows, int max_len, int plane
   // workgroup a CU, 182 with four; 32 rows over 2048 tokens: 17 us, 22 with 8 tiles).
   const int width = chunk ? 128 : 32;
   const int blocks = B * hkv * ((cols + width - 1) / width);
-  const int least = chunk ? 4 * KT : DEC_NW * KT;
-  const int most = std::max(1, (max_len + least - 1) / least);
+  const int most = std::max(1, (max_len + SPAN_MIN - 1) / SPAN_MIN);
   int want = chunk ? 512 / std::max(1, std::min(blocks, 512)) : (255 + blocks) / blocks;
-  if (!chunk || B > 1) want = std::max(want, (max_len + 4095) / 4096);
-  p.chunk = chunk;
+  // rows <= B max_rows: no limit, as blocks >= rows hq / width.  Rows behind the last
+  // sequence have places in the workspace, too, so many of them mean fewer splits.
+  want = (int)std::min<long long>(want, 1 + (long long)split_room(hkv * G, cols) / rows);
+  if (!chunk || B > 1) want = std::max(want, (max_len + SPAN_MAX - 1) / SPAN_MAX);
   p.nsplit = std::max(1, std::min(want, most));
   p.span = ((max_len + p.nsplit - 1) / p.nsplit + KT - 1) / KT * KT;
   return p;
+}
+
+// Largest rows * nsplit (with nsplit > 1) of a plan with at most these rows and lengths.
+long long paged_split_rows(int hq, int G, int rows, int max_rows, int max_len) {
+  const long long room = split_room(hq, max_rows * G);
+  const long long len = (max_len + SPAN_MAX - 1) / SPAN_MAX;
+  const long long n = std::max(std::min<long long>(rows, room) + room, len > 1 ? rows * len : 0);
+  return max_len <= SPAN_MIN ? 0 : std::min(n, (long long)rows * ((max_len + SPAN_MIN - 1) / SPAN_MIN));
 }
 
 void paged_attention(const PagedAttn& a_, hipStream_t st) {

@@ -56,6 +56,7 @@ class DeviceModel:
     def __init__(self, cfg, n_max: int, gamma_max: int = 8, m_rounds: int = 5,
                  cap_max: int = 256, prefill_chunk: int = 256, device: str = "cuda:0",
                  cache: str = "flat"):
+        _need(cache in ("flat", "bf16", "e4m3"), "cache must be 'flat', 'bf16' or 'e4m3'")
         self.cfg = cfg
         self.dev = torch.device(device)
         self.bf = cfg.dtype == "bf16"
@@ -445,6 +446,11 @@ def _here(dev: torch.device, f, *args):
             f(*args, s)
 
 
+def _need_workspace(w: torch.Tensor, dev: torch.device):
+    _need(w.dtype == torch.uint8 and w.is_contiguous() and w.device == dev,
+          "workspace must be dense uint8 on the same device")
+
+
 _DT = {torch.float32: K.KS_F32, torch.bfloat16: K.KS_BF16}
 
 
@@ -469,6 +475,7 @@ def sample_draw(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=N
     """One token per row of logits [rows, vocab] (float32 or bfloat16) from the given
     uniforms u [rows], with every row's own settings (tensors [rows], None: 1 or off):
     see ks_sample_draw.  Fills tokens (returned), logprob and kept where given."""
+    _need(logits.dim() == 2 and u is not None, "logits must be [rows, vocab] and u given")
     R, V = logits.shape
     dev = logits.device
     _need(logits.dtype in _DT and logits.stride(1) == 1 and dev.type == "cuda",
@@ -483,6 +490,7 @@ def sample_draw(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=N
               "device: int32 top_k, tokens and kept, float32 the others")
     if workspace is None:
         workspace = sample_draw_workspace(R, V, dev)
+    _need_workspace(workspace, dev)
     p = lambda t: None if t is None else _ptr(t)  # noqa: E731
     s = K.DrawParams(p(temperature), p(top_k), p(top_p), p(min_p), _ptr(u))
     _here(dev, K.ks_sample_draw, _ptr(logits), _DT[logits.dtype], R, V,
@@ -625,6 +633,7 @@ def paged_attention(cache: PagedCache, table, row_start, pos0, q, scale: float |
     r = _paged_rows(cache, table, row_start, pos0, rows, max_rows, max_len, err)
     if workspace is None:
         workspace = paged_attention_workspace(cache, r.B, rows, hq, r.max_rows, r.max_len)
+    _need_workspace(workspace, cache.device)
     _here(cache.device, K.ks_paged_attention, cache.ref, C.byref(r), _ptr(q), ldq, _ptr(out), ldo,
           hq, _DT[q.dtype], cache.hd ** -0.5 if scale is None else scale,
           None if lse is None else _ptr(lse), _ptr(workspace), workspace.numel())

@@ -582,3 +582,23 @@ def test_table_rows_of_a_wider_table_and_strided_rows(E):
                 lambda: E.paged_append(x.cache, i32(x.table), rs, p0.cpu(), k, v)):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_one_workspace_for_smaller_calls(E):
+    """A workspace for many sequences takes one long one, split more finely, and rows
+    behind the last sequence, which have places in it; the same results as with its own."""
+    x = Case(E, 3, 32, 2, 128, 64, 16, "e4m3", "bf16", 40, seed=14)
+    x.step([2400, 70, 30], check=False)
+    (q, _, _), _ = x.rows(64)
+    ws = E.paged_attention_workspace(x.cache, 64, 64, 32, 64, 2560)
+    for rows, rs, at in ((64, [0, 40], [2360]), (64, [0, 1], [2399]), (3, [0, 3], [2397]),
+                         (64, [0, 1, 33], [2399, 38]), (1, [0, 1], [2399])):
+        n = len(at)
+        for m in (None, max(np.diff(rs))):
+            a = [i32(x.table[:n]), i32(rs), i32(at), q[:rows].contiguous()]
+            out = torch.full_like(a[3], 7.0)
+            lse = torch.zeros(rows, 32, device="cuda")
+            E.paged_attention(x.cache, *a, out=out, lse=lse, max_rows=m, workspace=ws)
+            own = E.paged_attention(x.cache, *a, max_rows=m, out=torch.full_like(out, 7.0))
+            assert torch.equal(out, own) and bool((out[rs[-1]:] == 7).all())
+            x.check_attention(a[3][:rs[-1]], out[:rs[-1]], lse[:rs[-1]], rs, at)

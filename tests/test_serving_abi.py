@@ -1,6 +1,7 @@
 """Refusals of the paged cache and draw calls, before any launch (no GPU)."""
 import ctypes as C
 
+import numpy as np
 import pytest
 
 from paper_2602_20217_amd import _lib as K
@@ -127,3 +128,23 @@ def test_bad_draw():
     assert e.value.status == K.KS_ENOMEM
     for bad in ((-1, 1000), (65536, 1000), (4, 0), (4, 524289)):
         assert K.ks_sample_draw_workspace_bytes(*bad) == 0
+
+
+@pytest.mark.parametrize("hkv,G", [(1, 1), (2, 4), (8, 4), (8, 1), (1, 128), (4, 16)])
+def test_workspace_of_bounds_is_enough_below_them(hkv, G):
+    """Fewer sequences, rows or positions than a workspace was asked for never need more,
+    though they may be split more finely."""
+    rng = np.random.RandomState(hkv * G)
+    c = cache(hkv=hkv)
+    f = lambda *a: K.ks_paged_attention_workspace_bytes(C.byref(c), a[0], a[1], hkv * G, *a[2:])
+    for _ in range(500):
+        top = [int(2 ** rng.uniform(0, e)) for e in (8, 12, 11, 18)]
+        for _ in range(10):
+            low = [rng.randint(1, t + 1) for t in top]
+            assert f(*low) <= f(*top), (top, low)
+
+
+def test_cache_kinds():
+    from paper_2602_20217_amd.engine import DeviceModel
+    with pytest.raises(ValueError, match="cache must be"):
+        DeviceModel(None, 128, cache="fp8")
