@@ -435,19 +435,20 @@ def _need(ok: bool, msg: str):
         raise ValueError(msg)
 
 
-def _here(dev: torch.device, f, *args):
-    """Calls f with args and the current stream of dev, dev being current."""
-    i = dev.index
-    s = torch._C._cuda_getCurrentRawStream(i)  # current_stream() builds an object: 2.8 us
-    if i == torch.cuda.current_device():
+def _here(at: int, f, *args):
+    """Calls f with args and the current stream of GPU at, it being current.  (These calls
+    take a few microseconds on the GPU, and so their checks look at devices by index and
+    build their messages only when they fail.)"""
+    s = torch._C._cuda_getCurrentRawStream(at)  # current_stream() builds an object: 2.8 us
+    if at == torch._C._cuda_getDevice():
         f(*args, s)
     else:
-        with torch.cuda.device(dev):
+        with torch.cuda.device(at):
             f(*args, s)
 
 
-def _need_workspace(w: torch.Tensor, dev: torch.device):
-    _need(w.dtype == torch.uint8 and w.is_contiguous() and w.device == dev,
+def _need_workspace(w: torch.Tensor, at: int):
+    _need(w.dtype is torch.uint8 and w.is_contiguous() and w.get_device() == at,
           "workspace must be dense uint8 on the same device")
 
 
@@ -456,11 +457,12 @@ _DT = {torch.float32: K.KS_F32, torch.bfloat16: K.KS_BF16}
 
 def _rows3(t: torch.Tensor, heads: int, hd: int, name: str) -> int:
     """Row stride (elements) of t [rows, heads, hd], dense inside a row."""
-    n, h, d = t.shape if t.dim() == 3 else (0, 0, 0)
-    ld, sh, sd = t.stride() if t.dim() == 3 else (0, 0, 0)
-    if h != heads or d != hd or n and (sd != 1 or heads != 1 and sh != hd):
-        raise ValueError(f"{name} must be [rows, {heads}, {hd}], dense rows")
-    return ld if n > 1 else max(ld, heads * hd)
+    shape = t.shape
+    if len(shape) == 3 and shape[1] == heads and shape[2] == hd:
+        n, (ld, sh, sd) = shape[0], t.stride()
+        if n == 0 or sd == 1 and (heads == 1 or sh == hd):
+            return ld if n > 1 else max(ld, heads * hd)
+    raise ValueError(f"{name} must be [rows, {heads}, {hd}], dense rows")
 
 
 def sample_draw_workspace(rows: int, vocab: int, device="cuda") -> torch.Tensor:
@@ -476,26 +478,32 @@ def sample_draw(logits: torch.Tensor, u: torch.Tensor, temperature=None, top_k=N
     uniforms u [rows], with every row's own settings (tensors [rows], None: 1 or off):
     see ks_sample_draw.  Fills tokens (returned), logprob and kept where given."""
     _need(logits.dim() == 2 and u is not None, "logits must be [rows, vocab] and u given")
-    R, V = logits.shape
-    dev = logits.device
-    _need(logits.dtype in _DT and logits.stride(1) == 1 and dev.type == "cuda",
+    shape, at = logits.shape, logits.get_device()
+    R, V = shape
+    row = shape[:1]
+    ld, step = logits.stride()
+    _need(logits.dtype in _DT and step == 1 and at >= 0,
           "logits must be float32 or bfloat16 [rows, vocab] on a GPU, dense rows")
     if tokens is None:
-        tokens = torch.empty(R, dtype=torch.int32, device=dev)
-    for t, dt in ((u, torch.float32), (temperature, torch.float32), (top_k, torch.int32),
-                  (top_p, torch.float32), (min_p, torch.float32), (tokens, torch.int32),
-                  (logprob, torch.float32), (kept, torch.int32)):
-        _need(t is None or t.shape == (R,) and t.dtype == dt and t.is_contiguous()
-              and t.device == dev, f"settings and results must be dense [{R}] on the logits' "
-              "device: int32 top_k, tokens and kept, float32 the others")
+        tokens = torch.empty(R, dtype=torch.int32, device=logits.device)
+    f32, i32 = torch.float32, torch.int32
+    ptr = []
+    for t, dt in ((temperature, f32), (top_k, i32), (top_p, f32), (min_p, f32), (u, f32),
+                  (tokens, i32), (logprob, f32), (kept, i32)):
+        if t is None:
+            ptr.append(None)
+            continue
+        if (t.dtype is not dt or t.shape != row or not t.is_contiguous()
+                or t.get_device() != at):
+            raise ValueError(f"settings and results must be dense [{R}] on the logits' device: "
+                             "int32 top_k, tokens and kept, float32 the others")
+        ptr.append(t.data_ptr())
     if workspace is None:
-        workspace = sample_draw_workspace(R, V, dev)
-    _need_workspace(workspace, dev)
-    p = lambda t: None if t is None else _ptr(t)  # noqa: E731
-    s = K.DrawParams(p(temperature), p(top_k), p(top_p), p(min_p), _ptr(u))
-    _here(dev, K.ks_sample_draw, _ptr(logits), _DT[logits.dtype], R, V,
-          logits.stride(0) if R > 1 else V, C.byref(s), _ptr(tokens), p(logprob), p(kept),
-          _ptr(workspace), workspace.numel())
+        workspace = sample_draw_workspace(R, V, logits.device)
+    _need_workspace(workspace, at)
+    s = K.DrawParams(*ptr[:5])
+    _here(at, K.ks_sample_draw, logits.data_ptr(), _DT[logits.dtype], R, V, ld if R > 1 else V,
+          C.byref(s), *ptr[5:], workspace.data_ptr(), workspace.numel())
     return tokens
 
 
@@ -545,7 +553,7 @@ class PagedCache:
         _need(all(t.is_contiguous() and t.device == k.device for t in ts),
               "cache tensors must be contiguous and on one device")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.device = k.device
+        self.device, self.at = k.device, k.get_device()
         self.page, self.block, self.hkv, self.hd = page, block, hkv, hd
         self.desc = K.PagedCache(_ptr(k), _ptr(v), _ptr(k_scale) if e4 else None,
                                  _ptr(v_scale) if e4 else None, n, page, block, hkv, hd,
@@ -554,25 +562,24 @@ class PagedCache:
 
 
 def _paged_rows(cache: PagedCache, table, row_start, pos0, rows, max_rows, max_len, err):
-    B = pos0.shape[0]
-    i32 = torch.int32
-    _need(table.dim() == 2 and table.shape[0] == B and table.dtype == i32
-          and table.stride(1) == 1 and table.device == cache.device,
+    B, width = table.shape if table.dim() == 2 else (-1, 0)
+    ld, step = table.stride() if table.dim() == 2 else (0, 0)
+    i32, at = torch.int32, cache.at
+    _need(B >= 0 and pos0.shape == (B,) and table.dtype is i32 and step == 1
+          and table.get_device() == at,
           "table must be int32 [B, pages], dense rows, on the cache's device")
-    _need(row_start.shape == (B + 1,) and row_start.dtype == i32 and row_start.is_contiguous()
-          and pos0.dtype == i32 and pos0.is_contiguous() and pos0.device == cache.device
-          and row_start.device == cache.device,
+    _need(row_start.shape == (B + 1,) and row_start.dtype is i32 and row_start.is_contiguous()
+          and pos0.dtype is i32 and pos0.is_contiguous() and pos0.get_device() == at
+          and row_start.get_device() == at,
           "row_start must be int32 [B + 1] and pos0 int32 [B], on the cache's device")
     if err is not None:
-        _need(err.shape == (B,) and err.dtype == i32 and err.is_contiguous()
-              and err.device == cache.device, "err must be int32 [B] on the cache's device")
-    width = table.shape[1]
+        _need(err.shape == (B,) and err.dtype is i32 and err.is_contiguous()
+              and err.get_device() == at, "err must be int32 [B] on the cache's device")
     most = width * cache.page
-    return K.PagedRows(B, rows, _ptr(row_start), _ptr(pos0), _ptr(table),
-                       table.stride(0) if B > 1 else width,
-                       rows if max_rows is None else max_rows,
+    return K.PagedRows(B, rows, row_start.data_ptr(), pos0.data_ptr(), table.data_ptr(),
+                       ld if B > 1 else width, rows if max_rows is None else max_rows,
                        most if max_len is None else min(max_len, most),
-                       None if err is None else _ptr(err))
+                       None if err is None else err.data_ptr())
 
 
 def paged_append(cache: PagedCache, table, row_start, pos0, k, v, q=None, rope=None, q_out=None,
@@ -580,29 +587,32 @@ def paged_append(cache: PagedCache, table, row_start, pos0, k, v, q=None, rope=N
     """Stores the rows' keys (rotated by rope [positions, hd/2, 2]) and values and
     returns the rotated queries (in q_out, by default a new tensor; None without q).
     See ks_paged_append; row strides are free, so slices of a fused projection do."""
-    hkv, hd, rows = cache.hkv, cache.hd, k.shape[0]
+    hkv, hd, rows, at, dt = cache.hkv, cache.hd, k.shape[0], cache.at, k.dtype
     ldk, ldv = _rows3(k, hkv, hd, "k"), _rows3(v, hkv, hd, "v")
-    _need(k.dtype in _DT and v.dtype == k.dtype and v.shape[0] == rows
-          and k.device == cache.device and v.device == cache.device,
+    _need(dt in _DT and v.dtype is dt and v.shape[0] == rows
+          and k.get_device() == at and v.get_device() == at,
           "k and v must be float32 or bfloat16, of the same rows, on the cache's device")
     hq = ldq = ldo = 0
+    pq = po = pr = None
     if q is not None:
         hq = q.shape[1]
         ldq = _rows3(q, hq, hd, "q")
         if q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         ldo = _rows3(q_out, hq, hd, "q_out")
-        _need(q.dtype == k.dtype and q_out.dtype == k.dtype and q.shape[0] == rows
-              and q_out.shape[0] == rows and q.device == cache.device
-              and q_out.device == cache.device, "q and q_out must match k")
+        _need(q.dtype is dt and q_out.dtype is dt and q.shape[0] == rows
+              and q_out.shape[0] == rows and q.get_device() == at
+              and q_out.get_device() == at, "q and q_out must match k")
+        pq, po = q.data_ptr(), q_out.data_ptr()
+    n = 0
     if rope is not None:
-        _need(rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2) and rope.dtype == torch.float32
-              and rope.is_contiguous() and rope.device == cache.device,
+        _need(rope.dim() == 3 and rope.shape[1:] == (hd // 2, 2) and rope.dtype is torch.float32
+              and rope.is_contiguous() and rope.get_device() == at,
               "rope must be float32 [positions, hd / 2, 2] on the cache's device")
+        pr, n = rope.data_ptr(), rope.shape[0]
     r = _paged_rows(cache, table, row_start, pos0, rows, max_rows, None, err)
-    _here(cache.device, K.ks_paged_append, cache.ref, C.byref(r), None if q is None else _ptr(q),
-          ldq, _ptr(k), ldk, _ptr(v), ldv, None if q is None else _ptr(q_out), ldo, hq,
-          _DT[k.dtype], None if rope is None else _ptr(rope), 0 if rope is None else rope.shape[0])
+    _here(at, K.ks_paged_append, cache.ref, C.byref(r), pq, ldq, k.data_ptr(), ldk, v.data_ptr(),
+          ldv, po, ldo, hq, _DT[dt], pr, n)
     return q_out if q is not None else None
 
 
@@ -619,22 +629,22 @@ def paged_attention(cache: PagedCache, table, row_start, pos0, q, scale: float |
     """Causal attention of the rows q [rows, hq, hd] over their sequences' pages (see
     ks_paged_attention).  max_rows and max_len bound the rows and positions of a
     sequence; they default to what the shapes allow, and tight ones are faster."""
-    rows, hq = q.shape[0], q.shape[1]
+    rows, hq, at, dt = q.shape[0], q.shape[1], cache.at, q.dtype
     ldq = _rows3(q, hq, cache.hd, "q")
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(q.shape, dtype=dt, device=q.device)
     ldo = _rows3(out, hq, cache.hd, "out")
-    _need(q.dtype in _DT and out.dtype == q.dtype and out.shape[0] == rows
-          and q.device == cache.device and out.device == cache.device,
+    _need(dt in _DT and out.dtype is dt and out.shape[0] == rows
+          and q.get_device() == at and out.get_device() == at,
           "q and out must be float32 or bfloat16, of the same rows, on the cache's device")
     if lse is not None:
-        _need(lse.shape == (rows, hq) and lse.dtype == torch.float32 and lse.is_contiguous()
-              and lse.device == cache.device, "lse must be float32 [rows, hq]")
+        _need(lse.shape == (rows, hq) and lse.dtype is torch.float32 and lse.is_contiguous()
+              and lse.get_device() == at, "lse must be float32 [rows, hq]")
     r = _paged_rows(cache, table, row_start, pos0, rows, max_rows, max_len, err)
     if workspace is None:
         workspace = paged_attention_workspace(cache, r.B, rows, hq, r.max_rows, r.max_len)
-    _need_workspace(workspace, cache.device)
-    _here(cache.device, K.ks_paged_attention, cache.ref, C.byref(r), _ptr(q), ldq, _ptr(out), ldo,
-          hq, _DT[q.dtype], cache.hd ** -0.5 if scale is None else scale,
-          None if lse is None else _ptr(lse), _ptr(workspace), workspace.numel())
+    _need_workspace(workspace, at)
+    _here(at, K.ks_paged_attention, cache.ref, C.byref(r), q.data_ptr(), ldq, out.data_ptr(), ldo,
+          hq, _DT[dt], cache.hd ** -0.5 if scale is None else scale,
+          None if lse is None else lse.data_ptr(), workspace.data_ptr(), workspace.numel())
     return out
