@@ -1380,16 +1380,15 @@ __global__ __launch_bounds__(256, 2) void k_pg_chunk(PagedAttn a) {
   }
 }
 
-// NW waves per (row, query head) join the splits that hold keys of the row, each of
+// NW waves per (row, query head), U splits a wave at a time, join the splits that hold keys of the row, each of
 // them every NW-th, in order, then the waves' results.  Partials are (o[hd], max,
 // sum) with the maximum in natural units.  The first partials are requested before
 // the row's length is known (what they hold then is not used), so the loads of a
 // launch lie one memory latency deep, not three: 32 splits of one row's 32 heads 4.0 us
 // with four waves, 12.2 with one that asks for the length first.
-template <typename T, int HD, int NW>
+template <typename T, int HD, int NW, int U>
 __global__ __launch_bounds__(256) void k_pg_merge(PagedAttn a) {
   constexpr int DPL = HD / 64;
-  constexpr int U = 8;
   __shared__ float s_o[4][HD], s_m[4], s_l[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, w = wave % NW;
   const int job = blockIdx.x * (4 / NW) + wave / NW;
@@ -1585,13 +1584,20 @@ void paged_attention(const PagedAttn& a_, hipStream_t st) {
 #undef KS_ATT
 #undef KS_ATT_T
   if (!a.part || !a.out) return;
-  // up to eight splits are one wave's loads
+  // Up to eight splits are one wave's loads; as many as there may be, since the places of
+  // missing ones are loaded, too (64 sequences of 8000 tokens, 128 rows each, 2 splits:
+  // 1318 us, 1366 with eight loads).
   const int per = a.nsplit > 8 ? 1 : 4;  // (row, head) pairs of a workgroup
   const dim3 mgrid((unsigned)(((size_t)a.rows.rows * a.hq + per - 1) / per));
 #define KS_MRG(T_, HD_)                                                                 \
   do {                                                                                  \
-    if (per == 1) KS_LAUNCH((k_pg_merge<T_, HD_, 4>), mgrid, dim3(256), 0, st, a);      \
-    else KS_LAUNCH((k_pg_merge<T_, HD_, 1>), mgrid, dim3(256), 0, st, a);               \
+    if (per == 1) KS_LAUNCH((k_pg_merge<T_, HD_, 4, 8>), mgrid, dim3(256), 0, st, a);   \
+    else if (a.nsplit > 4)                                                              \
+      KS_LAUNCH((k_pg_merge<T_, HD_, 1, 8>), mgrid, dim3(256), 0, st, a);               \
+    else if (a.nsplit > 2)                                                              \
+      KS_LAUNCH((k_pg_merge<T_, HD_, 1, 4>), mgrid, dim3(256), 0, st, a);               \
+    else                                                                                \
+      KS_LAUNCH((k_pg_merge<T_, HD_, 1, 2>), mgrid, dim3(256), 0, st, a);               \
   } while (0)
   if (a.dtype == KS_BF16) {
     if (c.hd == 128) KS_MRG(bf16_t, 128);
